@@ -388,6 +388,90 @@ int grem_edge_list_cut(const int32_t *src, const int32_t *dst, int64_t m, const 
 int grem_edge_stream_profile_enable(int32_t on);
 int grem_edge_stream_profile_read(double *count_ms, int64_t *launches, int64_t *edges);
 
+/* ---- Layers on a partitioned graph --------------------------------------------------------------
+ *
+ * What a program runs on a graph and its partitions: the mean over the neighbours of the same partition, a
+ * matrix product with bias, activation and residual, layer norm, and activations kept in 8 bits between the
+ * forward and the backward pass.  Matrices are rows of values, the values of a row side by side, rows `ld*`
+ * values apart (ld >= the row's length; any base and stride that is a multiple of the value's size).  Every
+ * matrix, vector of parameters and gradient of a call is of one type; sums, statistics and accumulators are
+ * held in 32 bits and an output is rounded to its type once, to nearest even.  Gradients overwrite their
+ * outputs.  The calls only enqueue kernels: no read-back, no allocation, so they can be captured in a HIP
+ * graph; workspaces are the caller's, of at least the bytes the call's `_bytes` function names, aligned to 256 bytes, and not
+ * shared by calls that overlap in time.  Same arguments, same bytes: no atomics on values.
+ * Outputs must not overlap inputs, except that a matrix product's `out` may be its `residual`.
+ * Widths are at most 2^20, rows at most 2^30; rows may be 0 (parameters' gradients are then 0).
+ * Errors: GREM_ERR_ARG (null or misaligned pointer, a size or stride out of range, unknown type or
+ * activation), GREM_ERR_NOMEM (workspace missing or too small), GREM_ERR_HIP. */
+#define GREM_F32 0
+#define GREM_BF16 1
+#define GREM_F16 2
+
+/* Rows of values, or, where exponents is not NULL, of an 8-bit checkpoint: data are its codes (int8, stride
+ * in bytes) and exponents its exponent bytes, exponent_stride apart. */
+typedef struct grem_rows {
+    const void *data;
+    int64_t stride;
+    const uint8_t *exponents;
+    int64_t exponent_stride;
+} grem_rows;
+
+/* Mean of the neighbours' rows inside partitions: out[v] = sum of x[u] / |N(v)|, u in N(v) = the entries of
+ * row v whose label is v's own and not negative (labels: n int32, as a partition call leaves them; NULL = all
+ * entries count).  Entries are counted as stored.  out[v] = 0 where N(v) is empty; rows of x that no counted entry names
+ * are not read, whatever they hold.  counts_out: n int32, |N(v)|, or NULL.  nnz = rowptr[n], the length of colidx. */
+size_t grem_neighbour_mean_bytes(int64_t nnz, int64_t d);
+int grem_neighbour_mean(const void *rowptr, int32_t rowptr_bits, const int32_t *colidx, int64_t nnz, int64_t n,
+                        const int32_t *labels, int32_t type, int64_t d, const void *x, int64_t ldx, void *out,
+                        int64_t ldo, int32_t *counts_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradient: dx[u] = sum of dout[v] / counts[v] over the v with u in N(v).  rowptr_t, colidx_t: the transposed
+ * graph (a symmetric CSR is its own); counts: what the forward call left in counts_out. */
+int grem_neighbour_mean_backward(const void *rowptr_t, int32_t rowptr_bits, const int32_t *colidx_t, int64_t nnz,
+                                 int64_t n, const int32_t *labels, const int32_t *counts, int32_t type, int64_t d,
+                                 const void *dout, int64_t ldd, void *dx, int64_t lddx, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+/* z = [a | b] w^T + bias, out = act(z) + residual.  a: n x ka; b: n x kb or kb = 0; w: m x (ka + kb); bias: m
+ * values or NULL; residual: n x m or NULL; out: n x m; pre: n x m, receives z (rounded), or NULL. */
+#define GREM_ACT_NONE 0
+#define GREM_ACT_RELU 1
+#define GREM_ACT_GELU 2      /* z * Phi(z) */
+#define GREM_ACT_SILU 3      /* z / (1 + exp(-z)) */
+int grem_linear(int32_t type, int64_t n, int64_t m, const void *a, int64_t lda, int64_t ka, const void *b,
+                int64_t ldb, int64_t kb, const void *w, int64_t ldw, const void *bias, int32_t act,
+                const void *residual, int64_t ldr, void *out, int64_t ldo, void *pre, int64_t ldp, void *stream);
+
+/* dz = dout * act'(z) (ReLU's slope at 0 is 0), [da | db] = dz w, dw = dz^T [a | b], dbias = the columns' sums of
+ * dz; the residual's gradient is dout itself.  pre: z as grem_linear left it (unused without an activation).  a, b: the inputs, as they
+ * were or both as checkpoints; read for dw only.  Any of da, db, dw, dbias may be NULL.  dz is rounded to the type
+ * before the two products. */
+size_t grem_linear_backward_bytes(int32_t type, int64_t n, int64_t m, int64_t ka, int64_t kb, int32_t act);
+int grem_linear_backward(int32_t type, int64_t n, int64_t m, const void *dout, int64_t ldd, int32_t act,
+                         const void *pre, int64_t ldp, const grem_rows *a, int64_t ka, const grem_rows *b, int64_t kb,
+                         const void *w, int64_t ldw, void *da, int64_t ldda, void *db, int64_t lddb, void *dw,
+                         int64_t lddw, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Layer norm of every row: mean[v] = sum x / d, rstd[v] = 1 / sqrt(sum (x - mean)^2 / d + eps),
+ * y = (x - mean) rstd gamma + beta.  gamma, beta: d values or NULL (1 and 0); mean, rstd: n floats or NULL. */
+int grem_layer_norm(int32_t type, int64_t n, int64_t d, const void *x, int64_t ldx, const void *gamma,
+                    const void *beta, double eps, void *y, int64_t ldy, float *mean, float *rstd, void *stream);
+
+/* Its backward pass, from x (or a checkpoint of x) and the forward pass's mean and rstd.  dx, dgamma, dbeta may be NULL. */
+size_t grem_layer_norm_backward_bytes(int64_t n, int64_t d);
+int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, const void *dy, int64_t lddy, const grem_rows *x,
+                             const float *mean, const float *rstd, const void *gamma, void *dx, int64_t lddx,
+                             void *dgamma, void *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A checkpoint of n rows of d values: groups of 32 columns share an exponent byte.  e = the least whole number in
+ * [-130, 122] with |x| <= 127 * 2^e in the group; codes (int8) are x / 2^e to the nearest, ties to even, at most 63
+ * where 64 * 2^e would leave the type's range; the byte is e + 130.  A group that holds a NaN or an infinity has byte 255
+ * and codes 0, and is read back as NaN.  codes: n x d, ldc bytes apart; exponents: n x ceil(d / 32), lde apart.
+ * Read back, a code is code * 2^e: off by at most 2^(e-1), a 127th to a 254th of the group's largest value. */
+int grem_checkpoint_pack(int32_t type, int64_t n, int64_t d, const void *x, int64_t ldx, int8_t *codes, int64_t ldc,
+                         uint8_t *exponents, int64_t lde, void *stream);
+int grem_checkpoint_unpack(int32_t type, int64_t n, int64_t d, const grem_rows *x, void *y, int64_t ldy, void *stream);
+
 const char *grem_status_string(int code);
 const char *grem_kernel_name(int32_t kernel_class);
 

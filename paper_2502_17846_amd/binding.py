@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional, Union
 
 import torch
 
@@ -29,9 +29,15 @@ EXPORTS = [
     "grem_edge_stream_bipartition", "grem_edge_list_cut", "grem_edge_stream_profile_enable",
     "grem_edge_stream_profile_read", "grem_recursive_bisection", "grem_edge_buckets", "grem_expected_cut",
     "grem_expected_cut_noalloc", "grem_expected_cut_noalloc_max_n",
+    "grem_neighbour_mean_bytes", "grem_neighbour_mean", "grem_neighbour_mean_backward", "grem_linear",
+    "grem_linear_backward_bytes", "grem_linear_backward", "grem_layer_norm", "grem_layer_norm_backward_bytes",
+    "grem_layer_norm_backward", "grem_checkpoint_pack", "grem_checkpoint_unpack",
     "grem_plan_n", "grem_plan_neighbour_counts", "grem_plan_edge_cut", "grem_plan_expected_cut",
 ]
 EDGE_REFINE, EDGE_FIXED = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+CHECKPOINT_GROUP = 32        # columns that share an exponent byte
 
 
 class Options(ctypes.Structure):
@@ -50,6 +56,19 @@ def options(histogram_mode: int = 0, col_bits: int = 0, hub_degree: int = 0, lon
 
 def _opt(o):
     return None if o is None else ctypes.byref(o)
+
+
+class Rows(ctypes.Structure):
+    """grem_rows of include/grem.h: rows of values, or of a checkpoint's codes and exponent bytes."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64), ("exponents", ctypes.c_void_p),
+                ("exponent_stride", ctypes.c_int64)]
+
+
+class Checkpoint(NamedTuple):
+    """Rows kept in 8 bits: codes int8 (n, d), exponents uint8 (n, ceil(d / 32)), and the type they are read back as."""
+    codes: torch.Tensor
+    exponents: torch.Tensor
+    dtype: torch.dtype
 
 
 class GremError(RuntimeError):
@@ -143,6 +162,26 @@ def load():
     lib.grem_edge_stream_profile_enable.argtypes = [i32]
     lib.grem_edge_stream_profile_read.restype = ctypes.c_int
     lib.grem_edge_stream_profile_read.argtypes = [ctypes.POINTER(dbl), ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    size = ctypes.c_size_t
+    rows = ctypes.POINTER(Rows)
+    for name, res, args in (
+            ("grem_neighbour_mean_bytes", size, [i64, i64]),
+            ("grem_neighbour_mean", ctypes.c_int, [vp, i32, vp, i64, i64, vp, i32, i64, vp, i64, vp, i64, vp, vp, size, vp]),
+            ("grem_neighbour_mean_backward", ctypes.c_int,
+             [vp, i32, vp, i64, i64, vp, vp, i32, i64, vp, i64, vp, i64, vp, size, vp]),
+            ("grem_linear", ctypes.c_int,
+             [i32, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, vp]),
+            ("grem_linear_backward_bytes", size, [i32, i64, i64, i64, i64, i32]),
+            ("grem_linear_backward", ctypes.c_int,
+             [i32, i64, i64, vp, i64, i32, vp, i64, rows, i64, rows, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, size, vp]),
+            ("grem_layer_norm", ctypes.c_int, [i32, i64, i64, vp, i64, vp, vp, dbl, vp, i64, vp, vp, vp]),
+            ("grem_layer_norm_backward_bytes", size, [i64, i64]),
+            ("grem_layer_norm_backward", ctypes.c_int,
+             [i32, i64, i64, vp, i64, rows, vp, vp, vp, vp, i64, vp, vp, vp, size, vp]),
+            ("grem_checkpoint_pack", ctypes.c_int, [i32, i64, i64, vp, i64, vp, i64, vp, i64, vp]),
+            ("grem_checkpoint_unpack", ctypes.c_int, [i32, i64, i64, rows, vp, i64, vp])):
+        getattr(lib, name).restype = res
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -505,3 +544,222 @@ def grem_expected_cut_noalloc(rowptr, colidx, n, labels, x, out, stream=None) ->
 
 def grem_expected_cut_noalloc_max_n() -> int:
     return int(load().grem_expected_cut_noalloc_max_n())
+
+
+# ---- layers on a partitioned graph ------------------------------------------------------------------------------
+
+def _on(stream):
+    """What a call allocates (outputs, workspace) belongs to the stream that it runs on."""
+    return torch.cuda.stream(stream)
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a tensor on the GPU")
+    if t.dtype not in TYPES:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
+    return TYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor, dtype, shape, what: str):
+    """(pointer, values between rows) of a matrix whose rows' values lie side by side; rows may be any distance apart."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a tensor on the GPU")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    n, d = shape
+    if d > 1 and n > 0 and t.stride(1) != 1:
+        raise ValueError(f"the values of a row of {what} must lie side by side (strides {t.stride()})")
+    if n > 1 and t.stride(0) < d:
+        raise ValueError(f"the rows of {what} overlap (strides {t.stride()})")
+    return t.data_ptr(), max(t.stride(0), d) if n > 1 else d
+
+
+def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.numel() != count:
+        raise ValueError(f"{what} must have {count} entries, got shape {tuple(t.shape)}")
+    return _dev(t, dtype, what)
+
+
+def _width(t: Union[torch.Tensor, Checkpoint]) -> int:
+    return (t.codes if isinstance(t, Checkpoint) else t).shape[1]
+
+
+def _source(t: Union[torch.Tensor, Checkpoint], dtype, shape, what: str) -> Rows:
+    """grem_rows of a matrix or of a checkpoint of that shape and type."""
+    if not isinstance(t, Checkpoint):
+        p, ld = _matrix(t, dtype, shape, what)
+        return Rows(p, ld, None, 0)
+    if t.dtype != dtype:
+        raise TypeError(f"{what} is a checkpoint of {t.dtype}, not of {dtype}")
+    p, ld = _matrix(t.codes, torch.int8, shape, what + ".codes")
+    e, lde = _matrix(t.exponents, torch.uint8, (shape[0], -(-shape[1] // CHECKPOINT_GROUP)), what + ".exponents")
+    return Rows(p, ld, e, lde)
+
+
+def _like(out, shape, dtype, device, what: str):
+    """`out` checked, or a new matrix."""
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    return (out, *_matrix(out, dtype, shape, what))
+
+
+def _workspace(nbytes: int, device) -> tuple:
+    if nbytes == 0:
+        return None, None, 0
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return buf, buf.data_ptr(), nbytes
+
+
+def grem_neighbour_mean(rowptr, colidx, n, x, labels=None, out=None, stream=None):
+    """Returns (out (n, d), counts int32[n]): the mean over every vertex's neighbours of its own partition, and how many
+    they are; without labels over all neighbours."""
+    t = _type(x, "x")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    d = x.shape[1] if x.dim() == 2 else 0
+    px, ldx = _matrix(x, x.dtype, (n, d), "x")
+    if rowptr.numel() != n + 1:
+        raise ValueError(f"rowptr must have {n + 1} entries, got {rowptr.numel()}")
+    with _on(stream):
+        out, po, ldo = _like(out, (n, d), x.dtype, x.device, "out")
+        counts = torch.empty(n, dtype=torch.int32, device=x.device)
+        keep, ws, nbytes = _workspace(lib.grem_neighbour_mean_bytes(colidx.numel(), d), x.device)
+        rc = lib.grem_neighbour_mean(_dev(rowptr, rowptr.dtype, "rowptr"), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel(), n,
+                                     _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo, counts.data_ptr(), ws, nbytes,
+                                     stream.cuda_stream)
+    _check(rc, "grem_neighbour_mean")
+    return out, counts
+
+
+def grem_neighbour_mean_backward(rowptr_t, colidx_t, n, dout, counts, labels=None, dx=None, stream=None) -> torch.Tensor:
+    """dx (n, d) from dout and the forward call's counts; rowptr_t, colidx_t: the transposed graph (a symmetric one is its own)."""
+    t = _type(dout, "dout")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    d = dout.shape[1] if dout.dim() == 2 else 0
+    pd, ldd = _matrix(dout, dout.dtype, (n, d), "dout")
+    if rowptr_t.numel() != n + 1:
+        raise ValueError(f"rowptr_t must have {n + 1} entries, got {rowptr_t.numel()}")
+    with _on(stream):
+        dx, px, ldx = _like(dx, (n, d), dout.dtype, dout.device, "dx")
+        keep, ws, nbytes = _workspace(lib.grem_neighbour_mean_bytes(colidx_t.numel(), d), dout.device)
+        rc = lib.grem_neighbour_mean_backward(_dev(rowptr_t, rowptr_t.dtype, "rowptr_t"), _rowptr_bits(rowptr_t), _colidx(colidx_t),
+                                              colidx_t.numel(), n, _vector(labels, torch.int32, n, "labels"),
+                                              _vector(counts, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes,
+                                              stream.cuda_stream)
+    _check(rc, "grem_neighbour_mean_backward")
+    return dx
+
+
+def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, want_pre=False, stream=None):
+    """act([a | b] w^T + bias) + residual, (n, m); with want_pre also z = [a | b] w^T + bias, as (out, z)."""
+    t = _type(a, "a")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    if a.dim() != 2 or w.dim() != 2 or (b is not None and b.dim() != 2):
+        raise ValueError("a, b and w must be matrices")
+    n, ka, kb, m = a.shape[0], a.shape[1], 0 if b is None else b.shape[1], w.shape[0]
+    pa, lda = _matrix(a, a.dtype, (n, ka), "a")
+    pb, ldb = (None, 0) if b is None else _matrix(b, a.dtype, (n, kb), "b")
+    pw, ldw = _matrix(w, a.dtype, (m, ka + kb), "w")
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, a.dtype, (n, m), "residual")
+    with _on(stream):
+        out, po, ldo = _like(out, (n, m), a.dtype, a.device, "out")
+        z, pz, ldz = _like(None, (n, m), a.dtype, a.device, "pre") if want_pre else (None, None, 0)
+        rc = lib.grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, a.dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
+                             stream.cuda_stream)
+    _check(rc, "grem_linear")
+    return (out, z) if want_pre else out
+
+
+def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs=True, want_params=True, stream=None):
+    """Returns (da, db, dw, dbias); db is None without b, and so are the inputs' or the parameters' gradients that are not
+    wanted.  a, b: the forward call's inputs, or checkpoints of them; pre: its z (not used without an activation)."""
+    t = _type(dout, "dout")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    if dout.dim() != 2 or w.dim() != 2:
+        raise ValueError("dout and w must be matrices")
+    dtype, dev = dout.dtype, dout.device
+    n, m, ka, kb = dout.shape[0], dout.shape[1], _width(a), 0 if b is None else _width(b)
+    pd, ldd = _matrix(dout, dtype, (n, m), "dout")
+    pw, ldw = _matrix(w, dtype, (m, ka + kb), "w")
+    ra, rb = _source(a, dtype, (n, ka), "a"), None if b is None else _source(b, dtype, (n, kb), "b")
+    if act != ACT_NONE and pre is None:
+        raise ValueError("an activation's backward pass needs pre")
+    pz, ldz = _matrix(pre, dtype, (n, m), "pre") if act != ACT_NONE else (None, 0)
+    with _on(stream):
+        da, pda, ldda = _like(None, (n, ka), dtype, dev, "da") if want_inputs else (None, None, 0)
+        db, pdb, lddb = _like(None, (n, kb), dtype, dev, "db") if want_inputs and kb else (None, None, 0)
+        dw, pdw, lddw = _like(None, (m, ka + kb), dtype, dev, "dw") if want_params else (None, None, 0)
+        dbias = torch.empty(m, dtype=dtype, device=dev) if want_params else None
+        keep, ws, nbytes = _workspace(lib.grem_linear_backward_bytes(t, n, m, ka, kb, act), dev)
+        rc = lib.grem_linear_backward(t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb), kb,
+                                      pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes,
+                                      stream.cuda_stream)
+    _check(rc, "grem_linear_backward")
+    return da, db, dw, dbias
+
+
+def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
+    """Returns (y (n, d), mean float32[n], rstd float32[n])."""
+    t = _type(x, "x")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    n, d = x.shape if x.dim() == 2 else (0, 0)
+    px, ldx = _matrix(x, x.dtype, (n, d), "x")
+    with _on(stream):
+        out, po, ldo = _like(out, (n, d), x.dtype, x.device, "out")
+        mean, rstd = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
+        rc = lib.grem_layer_norm(t, n, d, px, ldx, _vector(gamma, x.dtype, d, "gamma"), _vector(beta, x.dtype, d, "beta"), float(eps), po,
+                                 ldo, mean.data_ptr(), rstd.data_ptr(), stream.cuda_stream)
+    _check(rc, "grem_layer_norm")
+    return out, mean, rstd
+
+
+def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params=True, stream=None):
+    """Returns (dx, dgamma, dbeta) (the last two None unless wanted); x: the forward call's input, or a checkpoint of it."""
+    t = _type(dy, "dy")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    n, d = dy.shape if dy.dim() == 2 else (0, 0)
+    pd, ldd = _matrix(dy, dy.dtype, (n, d), "dy")
+    rx = _source(x, dy.dtype, (n, d), "x")
+    with _on(stream):
+        dx, px, ldx = _like(dx, (n, d), dy.dtype, dy.device, "dx")
+        dgamma, dbeta = (torch.empty(d, dtype=dy.dtype, device=dy.device) if want_params else None for _ in range(2))
+        keep, ws, nbytes = _workspace(lib.grem_layer_norm_backward_bytes(n, d) if want_params else 0, dy.device)
+        rc = lib.grem_layer_norm_backward(t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, torch.float32, n, "mean"),
+                                          _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dy.dtype, d, "gamma"), px, ldx,
+                                          None if dgamma is None else dgamma.data_ptr(), None if dbeta is None else dbeta.data_ptr(),
+                                          ws, nbytes, stream.cuda_stream)
+    _check(rc, "grem_layer_norm_backward")
+    return dx, dgamma, dbeta
+
+
+def grem_checkpoint_pack(x, stream=None) -> Checkpoint:
+    """x's rows in 8 bits: groups of 32 columns, int8 codes and one exponent byte each."""
+    t = _type(x, "x")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    n, d = x.shape if x.dim() == 2 else (0, 0)
+    px, ldx = _matrix(x, x.dtype, (n, d), "x")
+    groups = -(-d // CHECKPOINT_GROUP)
+    with _on(stream):
+        codes = torch.empty((n, d), dtype=torch.int8, device=x.device)
+        exponents = torch.empty((n, groups), dtype=torch.uint8, device=x.device)
+        rc = lib.grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, stream.cuda_stream)
+    _check(rc, "grem_checkpoint_pack")
+    return Checkpoint(codes, exponents, x.dtype)
+
+
+def grem_checkpoint_unpack(checkpoint: Checkpoint, out=None, stream=None) -> torch.Tensor:
+    """The values that a checkpoint's codes stand for, in its type."""
+    n, d = checkpoint.codes.shape
+    if checkpoint.dtype not in TYPES:
+        raise TypeError(f"a checkpoint is read back as float32, bfloat16 or float16, not {checkpoint.dtype}")
+    rx = _source(checkpoint, checkpoint.dtype, (n, d), "checkpoint")
+    lib, stream = load(), stream or torch.cuda.current_stream()
+    with _on(stream):
+        out, po, ldo = _like(out, (n, d), checkpoint.dtype, checkpoint.codes.device, "out")
+        rc = lib.grem_checkpoint_unpack(TYPES[checkpoint.dtype], n, d, ctypes.byref(rx), po, ldo, stream.cuda_stream)
+    _check(rc, "grem_checkpoint_unpack")
+    return out

@@ -10,6 +10,8 @@ SRC = os.path.join(HERE, "csrc", "grem.hip")
 SRC_EDGE = os.path.join(HERE, "csrc", "grem_edge_stream.hip")
 SRC_BUCKETS = os.path.join(HERE, "csrc", "grem_edge_buckets.hip")
 SRC_EXPECTED = os.path.join(HERE, "csrc", "grem_expected_cut.hip")
+SRC_LAYERS = [os.path.join(HERE, "csrc", name) for name in
+              ("grem_neighbour_mean.hip", "grem_linear.hip", "grem_layer_norm.hip", "grem_checkpoint.hip")]
 LIB = os.path.join(HERE, "libgrem.so")
 
 FLAGS = [
@@ -22,7 +24,7 @@ FLAGS = [
 
 def build_library(verbose: bool = False, extra=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, *extra, "-o", LIB, SRC, SRC_EDGE, SRC_BUCKETS, SRC_EXPECTED]
+    cmd = [hipcc, *FLAGS, *extra, "-o", LIB, SRC, SRC_EDGE, SRC_BUCKETS, SRC_EXPECTED, *SRC_LAYERS]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

@@ -1,0 +1,132 @@
+"""The mean over the neighbours of the same partition and its gradient, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_17846_amd import binding as B
+from paper_2502_17846_amd import synth
+from tests import ref_layers as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _csr(rows, n, dtype):
+    """CSR of lists of columns."""
+    rowptr = np.zeros(n + 1, dtype)
+    rowptr[1:] = np.cumsum([len(r) for r in rows])
+    return rowptr, np.array([c for r in rows for c in r], np.int32)
+
+
+def _random(n, most, seed, dtype=np.int64, long_rows=()):
+    rng = np.random.default_rng(seed)
+    return _csr([rng.integers(0, n, dict(long_rows).get(v, int(rng.integers(0, most + 1)))) for v in range(n)], n, dtype)
+
+
+def _transposed(rowptr, colidx):
+    n = len(rowptr) - 1
+    rows = np.repeat(np.arange(n), np.diff(rowptr))
+    order = np.argsort(colidx, kind="stable")
+    out = np.zeros(n + 1, rowptr.dtype)
+    out[1:] = np.cumsum(np.bincount(colidx, minlength=n))
+    return out, rows[order].astype(np.int32)
+
+
+def _values(n, d, t, seed):
+    return torch.randn((n, d), generator=torch.Generator().manual_seed(seed)).to(t)
+
+
+def _check(rowptr, colidx, labels, x, dout, what):
+    t = x.dtype
+    n = len(rowptr) - 1
+    rp, ci, lab = torch.as_tensor(rowptr).to(DEV), torch.as_tensor(colidx).to(DEV), None if labels is None else torch.as_tensor(labels).to(DEV)
+    out, counts = B.grem_neighbour_mean(rp, ci, n, x if x.is_cuda else x.to(DEV), lab)
+    want, want_counts, tol = ref.neighbour_mean(rowptr, colidx, labels, x)
+    assert torch.equal(counts.cpu(), want_counts), what
+    ref.close(out, want, tol + ref.half_step(t) * (want.abs() + tol) + ref.least(t), what + " out")
+    tp, tc = _transposed(rowptr, colidx)
+    dx = B.grem_neighbour_mean_backward(torch.as_tensor(tp).to(DEV), torch.as_tensor(tc).to(DEV), n, dout if dout.is_cuda else dout.to(DEV), counts, lab)
+    want, tol = ref.neighbour_mean_backward(rowptr, colidx, labels, dout, want_counts)
+    ref.close(dx, want, tol + ref.half_step(t) * (want.abs() + tol) + ref.least(t), what + " dx")
+
+
+@pytest.mark.parametrize("t", ref.TYPES)
+@pytest.mark.parametrize("d", [1, 7, 16, 33, 64, 100, 129, 256, 300, 513, 1100])
+def test_widths(d, t):
+    rowptr, colidx = _random(60, 90, d)
+    labels = np.random.default_rng(d).integers(-1, 3, 60).astype(np.int32)
+    _check(rowptr, colidx, labels, _values(60, d, t, d), _values(60, d, t, d + 1), f"d={d}")
+
+
+@pytest.mark.parametrize("dtype", [np.int32, np.int64])
+@pytest.mark.parametrize("labelled", [False, True])
+def test_long_rows_are_split(dtype, labelled):
+    # rows around the length that a wave takes alone, and some of many segments
+    n = 40
+    rowptr, colidx = _random(n, 20, 5, dtype, [(0, 511), (3, 512), (4, 513), (7, 1024), (8, 1025), (20, 5000), (39, 40_000)])
+    labels = np.random.default_rng(1).integers(0, 2, n).astype(np.int32) if labelled else None
+    if labelled:
+        labels[4] = -1                                     # a long row without a partition: nothing counts
+    for d, t in ((48, torch.float32), (130, torch.bfloat16)):
+        _check(rowptr, colidx, labels, _values(n, d, t, d), _values(n, d, t, 1), f"long {d}")
+
+
+def test_rows_that_nothing_counts_in():
+    rows = [[], [1], [0, 1, 2], [3, 3], [0], [5, 0]]
+    rowptr, colidx = _csr(rows, 6, np.int32)
+    labels = np.array([0, 1, 1, -1, 2, 0], np.int32)
+    x = _values(6, 20, torch.float32, 0)
+    x[4], x[3] = float("nan"), float("inf")               # in no counted entry: never read
+    out, counts = B.grem_neighbour_mean(torch.as_tensor(rowptr).to(DEV), torch.as_tensor(colidx).to(DEV), 6, x.to(DEV), torch.as_tensor(labels).to(DEV))
+    assert counts.cpu().tolist() == [0, 1, 2, 0, 0, 2]
+    assert torch.equal(out.cpu()[[0, 3, 4]], torch.zeros((3, 20)))
+    assert torch.equal(out.cpu()[1], x[1])
+    ref.close(out[2:3], (x[1:2].double() + x[2:3].double()) / 2, 2.0 ** -22, "pair")
+
+
+def test_strides_and_odd_bases():
+    rowptr, colidx = _random(50, 30, 9)
+    labels = np.random.default_rng(2).integers(0, 2, 50).astype(np.int32)
+    for t in ref.TYPES:
+        wide = _values(100, 90, t, 3).to(DEV)
+        x, dout = wide[::2, 3:70], wide[1::2, 1:68]
+        _check(rowptr, colidx, labels, x, dout, "strided")
+
+
+def test_no_edges_one_vertex_no_vertices():
+    rp = torch.zeros(2, dtype=torch.int32, device=DEV)
+    ci = torch.empty(0, dtype=torch.int32, device=DEV)
+    out, counts = B.grem_neighbour_mean(rp, ci, 1, torch.ones((1, 9), device=DEV))
+    assert out.cpu().abs().sum() == 0 and counts.cpu().tolist() == [0]
+    out, counts = B.grem_neighbour_mean(rp[:1], ci, 0, torch.ones((0, 9), device=DEV))
+    assert out.shape == (0, 9)
+
+
+def test_offsets_beyond_32_bits():
+    # six rows 2^30 + 8 values apart: the last lies beyond 2^32 values and 10 GB
+    n, ld = 6, (1 << 30) + 8
+    big = torch.empty(n * ld, dtype=torch.bfloat16, device=DEV)
+    x = big.as_strided((n, 40), (ld, 1), 0)
+    x.copy_(_values(n, 40, torch.bfloat16, 4))
+    out = big.as_strided((n, 40), (ld, 1), 64)
+    rowptr, colidx = _csr([[5, 4], [0, 5], [3], [5], [], [5, 5, 1]], n, np.int64)
+    got, counts = B.grem_neighbour_mean(torch.as_tensor(rowptr).to(DEV), torch.as_tensor(colidx).to(DEV), n, x, out=out)
+    want, _, tol = ref.neighbour_mean(rowptr, colidx, None, x)
+    ref.close(got, want, tol + 2.0 ** -8 * want.abs(), "far rows")
+
+
+def test_the_same_bytes_every_time_and_on_another_stream():
+    g = synth.to_numpy(synth.rmat(14, 16, seed=3))
+    rp, ci = torch.as_tensor(g.rowptr).to(DEV), torch.as_tensor(g.colidx).to(DEV)
+    labels = B.grem_partition(rp, ci, g.n, 8, 1.05, 4096, 1)
+    x = _values(g.n, 128, torch.bfloat16, 8).to(DEV)
+    first, counts = B.grem_neighbour_mean(rp, ci, g.n, x, labels)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    again, _ = B.grem_neighbour_mean(rp, ci, g.n, x, labels, stream=side)
+    dx = B.grem_neighbour_mean_backward(rp, ci, g.n, x, counts, labels)
+    side.synchronize()
+    assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+    dx2 = B.grem_neighbour_mean_backward(rp, ci, g.n, x, counts, labels, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(dx.view(torch.int16), dx2.view(torch.int16))
