@@ -24,7 +24,7 @@ __device__ __forceinline__ int ck_byte(uint32_t most)
 // At the last binade of the type 64 * 2^e would be its 2^(largest exponent + 1): the codes stop at 63.
 template <class T> constexpr int ck_top() { return (__is_same(T, f16) ? 10 : 122) + kCkBias; }
 
-template <class T>
+template <class T, bool EVEN>
 __global__ __launch_bounds__(kCkBlock) void k_ck_pack(const T* __restrict__ x, int64_t ldx, int64_t n, int d, uint32_t per_row,
                                                       uint32_t rows, int8_t* __restrict__ codes, int64_t ldc,
                                                       uint8_t* __restrict__ exponents, int64_t lde)
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kCkBlock) void k_ck_pack(const T* __restrict__ x, i
         const uint32_t q = i / per_row, r = q < here ? q : here - 1;
         const int c = (int)(i - q * per_row) * kCkPer;
         float f[kCkPer];
-        load_floats<T, kCkPer>(x + (first + r) * ldx, c, d, f);
+        load_floats<T, kCkPer, EVEN>(x + (first + r) * ldx, c, d, f);
         uint32_t most = 0;
 #pragma unroll
         for (int j = 0; j < kCkPer; ++j) {
@@ -57,11 +57,11 @@ __global__ __launch_bounds__(kCkBlock) void k_ck_pack(const T* __restrict__ x, i
             const float v = rintf(ldexpf(f[j], kCkBias - byte));
             code[j] = byte == kCkNotFinite ? 0.0f : fminf(fmaxf(v, -limit), limit);
         }
-        store_floats<int8_t, kCkPer>(codes + (first + r) * ldc, c, d, code);
+        if (c < d) store_floats<int8_t, kCkPer, EVEN>(codes + (first + r) * ldc, c, d, code);
     }
 }
 
-template <class T>
+template <class T, bool EVEN>
 __global__ __launch_bounds__(kCkBlock) void k_ck_unpack(Rows x, int64_t n, int d, uint32_t per_row, uint32_t rows,
                                                         T* __restrict__ y, int64_t ldy)
 {
@@ -70,9 +70,11 @@ __global__ __launch_bounds__(kCkBlock) void k_ck_unpack(Rows x, int64_t n, int d
     for (uint32_t i = threadIdx.x; i < here * per_row; i += kCkBlock) {
         const uint32_t r = i / per_row;
         const int c = (int)(i - r * per_row) * kCkPer;
+        Held<T, true, kCkPer> h;
+        h.template load<EVEN>(x, first + r, c, d);
         float f[kCkPer];
-        load_row<T, true, kCkPer>(x, first + r, c, d, f);
-        if (c < d) store_floats<T, kCkPer>(y + (first + r) * ldy, c, d, f);
+        h.floats(f);
+        if (c < d) store_floats<T, kCkPer, EVEN>(y + (first + r) * ldy, c, d, f);
     }
 }
 
@@ -104,8 +106,10 @@ extern "C" int grem_checkpoint_pack(int32_t type, int64_t n, int64_t d, const vo
     const CkShape s = ck_shape(n, d);
     layer_typed(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((k_ck_pack<T>), dim3(s.grid), dim3(kCkBlock), 0, (hipStream_t)stream, (const T*)x, ldx, n, (int)d, s.per_row,
-                           s.rows, codes, ldc, exponents, lde);
+        layer_either(d % kCkPer == 0, [&](auto even) {
+            hipLaunchKernelGGL((k_ck_pack<T, decltype(even)::value>), dim3(s.grid), dim3(kCkBlock), 0, (hipStream_t)stream, (const T*)x, ldx, n,
+                               (int)d, s.per_row, s.rows, codes, ldc, exponents, lde);
+        });
     });
     return layer_launched();
 }
@@ -120,8 +124,10 @@ extern "C" int grem_checkpoint_unpack(int32_t type, int64_t n, int64_t d, const 
     const CkShape s = ck_shape(n, d);
     layer_typed(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((k_ck_unpack<T>), dim3(s.grid), dim3(kCkBlock), 0, (hipStream_t)stream, layer_rows(x), n, (int)d, s.per_row,
-                           s.rows, (T*)y, ldy);
+        layer_either(d % kCkPer == 0, [&](auto even) {
+            hipLaunchKernelGGL((k_ck_unpack<T, decltype(even)::value>), dim3(s.grid), dim3(kCkBlock), 0, (hipStream_t)stream, layer_rows(x), n,
+                               (int)d, s.per_row, s.rows, (T*)y, ldy);
+        });
     });
     return layer_launched();
 }

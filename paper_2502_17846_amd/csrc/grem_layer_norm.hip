@@ -30,17 +30,17 @@ template <int L> __device__ __forceinline__ float ln_sum(float x, float* sums)
     }
 }
 
-template <class T, int V> __device__ __forceinline__ void ln_param(const T* __restrict__ p, int c, int d, float none, float (&f)[V])
+template <class T, int V, bool EVEN = false> __device__ __forceinline__ void ln_param(const T* __restrict__ p, int c, int d, float none, float (&f)[V])
 {
     if (p) {
-        load_floats<T, V>(p, c, d, f);
+        load_floats<T, V, EVEN>(p, c, d, f);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = none;
     }
 }
 
-template <class T, int L, int C>
+template <class T, bool EVEN, int L, int C>
 __global__ __launch_bounds__(kLnBlock) void k_ln_forward(const T* __restrict__ x, int64_t ldx, int64_t n, int d,
                                                          const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
                                                          T* __restrict__ y, int64_t ldy, float* __restrict__ mean,
@@ -52,11 +52,14 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_forward(const T* __restrict__ x
     for (int64_t base = (int64_t)blockIdx.x * (kLnBlock / L); base < n; base += (int64_t)gridDim.x * (kLnBlock / L)) {
         const int64_t row = base + threadIdx.x / L;
         const int64_t r = row < n ? row : n - 1;
+        WordsOf<T, V> w[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) w[k] = load_words<T, V, EVEN>(x + r * ldx, (k * L + lane) * V, d);
         float f[C][V];
         float s = 0.0f;
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            load_floats<T, V>(x + r * ldx, (k * L + lane) * V, d, f[k]);
+            to_floats<T, V>(w[k], f[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += f[k][i];
         }
@@ -80,11 +83,11 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_forward(const T* __restrict__ x
             const int c = (k * L + lane) * V;
             if (c >= d) continue;
             float g[V], b[V];
-            ln_param<T, V>(gamma, c, d, 1.0f, g);
-            ln_param<T, V>(beta, c, d, 0.0f, b);
+            ln_param<T, V, EVEN>(gamma, c, d, 1.0f, g);
+            ln_param<T, V, EVEN>(beta, c, d, 0.0f, b);
 #pragma unroll
             for (int i = 0; i < V; ++i) f[k][i] = f[k][i] * rs * g[i] + b[i];
-            store_floats<T, V>(y + row * ldy, c, d, f[k]);
+            store_floats<T, V, EVEN>(y + row * ldy, c, d, f[k]);
         }
     }
 }
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_forward_wide(const T* __restric
 }
 
 // partial: per workgroup d sums of dy * xh, then d sums of dy
-template <class T, bool CK, int L, int C>
+template <class T, bool CK, bool EVEN, int L, int C>
 __global__ __launch_bounds__(kLnBlock) void k_ln_backward(const T* __restrict__ dy, int64_t lddy, Rows x, int64_t n, int d,
                                                           const float* __restrict__ mean, const float* __restrict__ rstd,
                                                           const T* __restrict__ gamma, T* __restrict__ dx, int64_t lddx,
@@ -153,13 +156,20 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_backward(const T* __restrict__ 
     for (int64_t base = (int64_t)blockIdx.x * R; base < n; base += (int64_t)gridDim.x * R) {
         const int64_t row = base + slot, r = row < n ? row : n - 1;
         const float mu = mean[r], rs = rstd[r];
+        WordsOf<T, V> wt[C];
+        Held<T, CK, V> wx[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            wt[k] = load_words<T, V, EVEN>(dy + r * lddy, (k * L + lane) * V, d);
+            wx[k].template load<EVEN>(x, r, (k * L + lane) * V, d);
+        }
         float xh[C][V], t[C][V];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             const int c = (k * L + lane) * V;
-            load_floats<T, V>(dy + r * lddy, c, d, t[k]);
-            load_row<T, CK, V>(x, r, c, d, xh[k]);
+            to_floats<T, V>(wt[k], t[k]);
+            wx[k].floats(xh[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 xh[k][i] = c + i < d ? (xh[k][i] - mu) * rs : 0.0f;
@@ -181,7 +191,7 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_backward(const T* __restrict__ 
             if (c >= d) continue;
 #pragma unroll
             for (int i = 0; i < V; ++i) t[k][i] = rs * (t[k][i] - s1 - xh[k][i] * s2);
-            if (dx) store_floats<T, V>(dx + row * lddx, c, d, t[k]);
+            if (dx) store_floats<T, V, EVEN>(dx + row * lddx, c, d, t[k]);
         }
     }
     if (!partial) return;
@@ -226,7 +236,9 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_backward_wide(const T* __restri
         auto pair = [&](int c, float (&t)[V], float (&xh)[V]) {
             float g[V];
             load_floats<T, V>(dy + row * lddy, c, d, t);
-            load_row<T, CK, V>(x, row, c, d, xh);
+            Held<T, CK, V> h;
+        h.template load<false>(x, row, c, d);
+        h.floats(xh);
             ln_param<T, V>(gamma, c, d, 1.0f, g);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -271,7 +283,9 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_columns_wide(const T* __restric
         const float mu = mean[r], rs = rstd[r];
         float t[V], xh[V];
         load_floats<T, V>(dy + r * lddy, c, d, t);
-        load_row<T, CK, V>(x, r, c, d, xh);
+        Held<T, CK, V> h;
+        h.template load<false>(x, r, c, d);
+        h.floats(xh);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             dg[i] += t[i] * ((xh[i] - mu) * rs);
@@ -352,8 +366,11 @@ extern "C" int grem_layer_norm(int32_t type, int64_t n, int64_t d, const void* x
         using T = decltype(t);
         const bool held = ln_shaped<T>(d, [&](auto shape) {
             constexpr int L = decltype(shape)::L, C = decltype(shape)::C;
-            hipLaunchKernelGGL((k_ln_forward<T, L, C>), dim3(ln_grid((n * L + kLnBlock - 1) / kLnBlock)), dim3(kLnBlock), 0, stream,
-                               (const T*)x, ldx, n, (int)d, (const T*)gamma, (const T*)beta, (float)eps, (T*)y, ldy, mean, rstd);
+            layer_either(d % kLnV<T> == 0, [&](auto even) {
+                hipLaunchKernelGGL((k_ln_forward<T, decltype(even)::value, L, C>), dim3(ln_grid((n * L + kLnBlock - 1) / kLnBlock)),
+                                   dim3(kLnBlock), 0, stream, (const T*)x, ldx, n, (int)d, (const T*)gamma, (const T*)beta, (float)eps, (T*)y,
+                                   ldy, mean, rstd);
+            });
         });
         if (!held)
             hipLaunchKernelGGL((k_ln_forward_wide<T>), dim3(ln_grid(n)), dim3(kLnBlock), 0, stream, (const T*)x, ldx, n, (int)d,
@@ -393,8 +410,10 @@ extern "C" int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, cons
                     constexpr int L = decltype(shape)::L, C = decltype(shape)::C;
                     const int64_t groups = (n * L + kLnBlock - 1) / kLnBlock;
                     parts = (int)(groups < kLnGroups ? groups : kLnGroups);
-                    hipLaunchKernelGGL((k_ln_backward<T, CK, L, C>), dim3((unsigned)parts), dim3(kLnBlock), 0, stream, (const T*)dy, lddy,
-                                       layer_rows(x), n, (int)d, mean, rstd, (const T*)gamma, (T*)dx, lddx, partial);
+                    layer_either(d % kLnV<T> == 0, [&](auto even) {
+                        hipLaunchKernelGGL((k_ln_backward<T, CK, decltype(even)::value, L, C>), dim3((unsigned)parts), dim3(kLnBlock), 0, stream,
+                                           (const T*)dy, lddy, layer_rows(x), n, (int)d, mean, rstd, (const T*)gamma, (T*)dx, lddx, partial);
+                    });
                 });
                 if (!held && dx)
                     hipLaunchKernelGGL((k_ln_backward_wide<T, CK>), dim3(ln_grid(n)), dim3(kLnBlock), 0, stream, (const T*)dy, lddy,

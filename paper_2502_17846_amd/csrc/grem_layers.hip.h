@@ -21,46 +21,61 @@ constexpr int64_t kLayerMaxRows = 1 << 30;
 constexpr int64_t kLayerMaxCols = 1 << 20;
 
 // A run of V values at the alignment of one: the hardware takes vector loads at any multiple of the element, so odd strides and
-// odd bases cost cache lines, not instructions.
-template <class T, int V> struct __attribute__((packed, aligned(alignof(T)))) Run { T v[V]; };
+// odd bases cost cache lines, not instructions.  It is loaded as whole words and taken apart afterwards: a run that may end
+// early has two ways of being loaded, and values that meet from two ways one by one are waited for where they meet.
+template <class T, int V> struct Words {
+    static constexpr int bytes = V * (int)sizeof(T), count = bytes / 4;
+    typedef uint32_t type __attribute__((ext_vector_type(count)));
+    struct __attribute__((packed, aligned(alignof(T)))) Place {
+        type w;
+    };
+};
 
-template <class T, int V> __device__ __forceinline__ void load_run(const T* __restrict__ p, T (&v)[V])
+template <class T, int V> using WordsOf = typename Words<T, V>::type;
+
+// values [c, c + V) of a row of d, zero from d on; EVEN: V divides d, so that a run is whole or absent
+template <class T, int V, bool EVEN> __device__ __forceinline__ WordsOf<T, V> load_words(const T* __restrict__ row, int c, int d)
 {
-    const Run<T, V> r = *(const Run<T, V>*)p;
+    using W = Words<T, V>;
+    if constexpr (EVEN) {
+        typename W::type w = {};
+        if (c < d) w = ((const typename W::Place*)(row + c))->w;
+        return w;
+    } else {
+        if (c + V <= d) return ((const typename W::Place*)(row + c))->w;
+        T v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = r.v[i];
+        for (int i = 0; i < V; ++i) v[i] = c + i < d ? row[c + i] : (T)0;
+        typename W::type w;
+        __builtin_memcpy(&w, v, W::bytes);
+        return w;
+    }
 }
 
-template <class T, int V> __device__ __forceinline__ void store_run(T* __restrict__ p, const T (&v)[V])
-{
-    Run<T, V> r;
-#pragma unroll
-    for (int i = 0; i < V; ++i) r.v[i] = v[i];
-    *(Run<T, V>*)p = r;
-}
-
-// values [c, c + V) of a row of d, as floats; zero from d on
-template <class T, int V> __device__ __forceinline__ void load_floats(const T* __restrict__ row, int c, int d, float (&f)[V])
+template <class T, int V> __device__ __forceinline__ void to_floats(const WordsOf<T, V>& w, float (&f)[V])
 {
     T v[V];
-    if (c + V <= d) {
-        load_run<T, V>(row + c, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = c + i < d ? row[c + i] : (T)0.0f;
-    }
+    __builtin_memcpy(v, &w, Words<T, V>::bytes);
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = (float)v[i];
 }
 
-// rounded to T, to nearest even: the one rounding of an output that is computed in 32 bits
-template <class T, int V> __device__ __forceinline__ void store_floats(T* __restrict__ row, int c, int d, const float (&f)[V])
+template <class T, int V, bool EVEN = false> __device__ __forceinline__ void load_floats(const T* __restrict__ row, int c, int d, float (&f)[V])
 {
+    to_floats<T, V>(load_words<T, V, EVEN>(row, c, d), f);
+}
+
+// rounded to T, to nearest even: the one rounding of an output that is computed in 32 bits
+template <class T, int V, bool EVEN = false> __device__ __forceinline__ void store_floats(T* __restrict__ row, int c, int d, const float (&f)[V])
+{
+    using W = Words<T, V>;
     T v[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = (T)f[i];
-    if (c + V <= d) {
-        store_run<T, V>(row + c, v);
+    if (EVEN || c + V <= d) {
+        typename W::type w;
+        __builtin_memcpy(&w, v, W::bytes);
+        ((typename W::Place*)(row + c))->w = w;
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -73,9 +88,12 @@ constexpr int kCkGroup = 32;
 constexpr int kCkBias = 130;
 constexpr int kCkNotFinite = 255;
 
-__device__ __forceinline__ float ck_value(int code, int byte)
+// 2^(byte - 130), NaN for a group that is not finite (whose codes are 0): code * scale is the value, exactly
+__device__ __forceinline__ float ck_scale(int byte)
 {
-    return byte == kCkNotFinite ? __builtin_nanf("") : ldexpf((float)code, byte - kCkBias);
+    // 2^(byte - 130) has exponent field byte - 3; from 3 down it is a number below the normal ones
+    const uint32_t bits = byte > 3 ? (uint32_t)(byte - 3) << 23 : 1u << (19 + byte);
+    return __uint_as_float(byte == kCkNotFinite ? 0x7FC00000u : bits);
 }
 
 // Rows of values, or of a checkpoint's codes and exponent bytes.
@@ -86,24 +104,34 @@ struct Rows {
     int64_t exponent_stride;
 };
 
-// values [c, c + V) of row r, in floats; V divides 32 and c is a multiple of V, so one exponent serves them all
-template <class T, bool CK, int V> __device__ __forceinline__ void load_row(const Rows& x, int64_t r, int c, int d, float (&f)[V])
-{
-    if constexpr (!CK) {
-        load_floats<T, V>((const T*)x.data + r * x.stride, c, d, f);
-    } else {
-        if (c >= d) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = 0.0f;
-            return;
-        }
-        const int byte = x.exponents[r * x.exponent_stride + c / kCkGroup];
-        float q[V];
-        load_floats<int8_t, V>((const int8_t*)x.data + r * x.stride, c, d, q);
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = c + i < d ? ck_value((int)q[i], byte) : 0.0f;
+// A run of a row on its way: its words, and the exponent byte where it is a checkpoint's (V divides 32 and c is a multiple of V, so one
+// serves the run).
+template <class T, bool CK, int V> struct Held {
+    WordsOf<T, V> w;
+    template <bool EVEN> __device__ __forceinline__ void load(const Rows& x, int64_t r, int c, int d)
+    {
+        w = load_words<T, V, EVEN>((const T*)x.data + r * x.stride, c, d);
     }
-}
+    __device__ __forceinline__ void floats(float (&f)[V]) const { to_floats<T, V>(w, f); }
+};
+
+template <class T, int V> struct Held<T, true, V> {
+    WordsOf<int8_t, V> w;
+    int byte;
+    template <bool EVEN> __device__ __forceinline__ void load(const Rows& x, int64_t r, int c, int d)
+    {
+        byte = kCkBias;
+        if (c < d) byte = x.exponents[r * x.exponent_stride + c / kCkGroup];
+        w = load_words<int8_t, V, EVEN>((const int8_t*)x.data + r * x.stride, c, d);
+    }
+    __device__ __forceinline__ void floats(float (&f)[V]) const
+    {
+        const float scale = ck_scale(byte);
+        to_floats<int8_t, V>(w, f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] *= scale;
+    }
+};
 
 // sum over groups of W neighbouring lanes, in every lane of the group
 template <int W> __device__ __forceinline__ float lanes_sum(float x)
@@ -143,6 +171,12 @@ template <class F> inline void layer_typed(int32_t type, F f)
     if (type == GREM_F32) f(float{});
     else if (type == GREM_BF16) f(bf16{});
     else f(f16{});
+}
+
+template <class F> inline void layer_either(bool even, F f)
+{
+    if (even) f(std::true_type{});
+    else f(std::false_type{});
 }
 
 }  // namespace

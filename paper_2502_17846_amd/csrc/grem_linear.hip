@@ -33,27 +33,49 @@ template <class T> __device__ __forceinline__ void mma(f32x4& acc, u32x4 a, u32x
 }
 
 // ---- activations ---------------------------------------------------------------------------------------------------------
+//
+// exp(-z^2/2) and the normal distribution function: Phi(|z|) = 1 - exp(-z^2/2) * (b1 t + .. + b5 t^5), t = 1 / (1 + q |z|)
+// (Abramowitz and Stegun, 26.2.17 / 7.1.26 at z / sqrt 2: off by at most 7.5e-8).  The math library's erfc takes three times the
+// instructions, and with them an epilogue's time outgrew its product's (262,144 x 512 by 256: 280 us with it, 200 without).
+struct Normal {
+    float density, below;           // exp(-z^2/2), Phi(z)
+};
+
+__device__ __forceinline__ Normal normal_at(float z)
+{
+    const float x = fabsf(z), t = __builtin_amdgcn_rcpf(1.0f + 0.2316419f * x);
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    const float poly = t * (0.31938153f + t * (-0.356563782f + t * (1.781477937f + t * (-1.821255978f + t * 1.330274429f))));
+    const float tail = 0.39894228040143268f * e * poly;
+    return Normal{e, z > 0.0f ? 1.0f - tail : tail};
+}
+
+// 1 / (1 + exp(-z)): 0 and 1 at the ends, where exp leaves its range
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
+
 template <int ACT> __device__ __forceinline__ float act(float z)
 {
     if constexpr (ACT == GREM_ACT_RELU) return z > 0.0f ? z : z == z ? 0.0f : z;
-    if constexpr (ACT == GREM_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    if constexpr (ACT == GREM_ACT_SILU) return z / (1.0f + expf(-z));
+    if constexpr (ACT == GREM_ACT_GELU) return z * normal_at(z).below;
+    if constexpr (ACT == GREM_ACT_SILU) return z * sigmoid(z);
     return z;
 }
 
 template <int ACT> __device__ __forceinline__ float act_slope(float z)
 {
     if constexpr (ACT == GREM_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-    if constexpr (ACT == GREM_ACT_GELU)
-        return 0.5f * erfcf(-0.70710678118654752f * z) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if constexpr (ACT == GREM_ACT_GELU) {
+        const Normal a = normal_at(z);
+        return a.below + z * 0.39894228040143268f * a.density;
+    }
     if constexpr (ACT == GREM_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-z));
+        const float s = sigmoid(z);
         return s * (1.0f + z * (1.0f - s));
     }
     return 1.0f;
 }
 
-template <class F> void by_act(int32_t a, F f)
+template <class F> __host__ __device__ __forceinline__ void by_act(int32_t a, F f)
 {
     switch (a) {
         case GREM_ACT_RELU: f(std::integral_constant<int, GREM_ACT_RELU>{}); break;
@@ -71,12 +93,12 @@ template <class F> void by_act(int32_t a, F f)
 // spread over the banks.
 //
 // The weights are the first operand: an accumulator's four registers then run along a row of the output, and which feature stands in
-// which row of the operand is free: tile i, row 4g + r is feature 4 * tiles * g + 4 i + r of the wave's, so that a lane's
-// features are side by side and leave in 16-byte stores.
+// which row of the operand is free: a lane gets runs of V features (16 bytes) whose four neighbours' runs lie beside its own, so that a
+// store instruction writes 64 bytes of each of 16 rows.
 struct Product {
     const void *a, *b, *w;
     int64_t lda, ldb, ldw, n;
-    int ka, kb, m;
+    int ka, kb, m, tiles_m;
 };
 
 struct Epilogue {
@@ -84,41 +106,158 @@ struct Epilogue {
     void *out, *pre;                // features [0, split) of a row
     void *out2;                     // features from split on
     int64_t ldr, ldo, ldp, ldo2;
-    int split;
+    int split, act;
 };
 
 constexpr int kLinBlock = 256;
 constexpr int kLinStep = 128;       // bytes
 
-// 16 bytes of a row's values from k on, zero from d on
-template <class T> __device__ __forceinline__ u32x4 chunk_of(const T* row, int k, int d)
+// BM rows (of the output's n, or features of dz) by BN, of which a wave takes WM by WN
+template <int BM_, int BN_, int WM_, int WN_, int STAGES = 2, int HALVES = 2> struct LinTile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, stages = STAGES, halves = HALVES, threads = BM / WM * (BN / WN) * 64;
+};
+
+// Workgroups go to the eight chiplets in turn.  Those that share a block of rows are given numbers eight apart, so that they run on
+// one chiplet and the rows come from its L2.
+struct LinPlace {
+    int64_t row;
+    int col;
+};
+
+__device__ __forceinline__ LinPlace lin_place(int cols)
+{
+    const uint32_t id = blockIdx.x, chiplet = id & 7u, local = id >> 3;
+    return LinPlace{(int64_t)(local / (uint32_t)cols) * 8 + chiplet, (int)(local % (uint32_t)cols)};
+}
+
+// 16 bytes at the alignment of a value
+struct __attribute__((packed, aligned(2))) Chunk {
+    u32x4 v;
+};
+
+// 16 bytes of a row's values from k on, zero from d on; WHOLE: the caller knows that they end before d.  (Where that is
+// known for all lanes there must be no branch on it: the two ways' values would meet element by element, which waits for the load.)
+template <class T, bool WHOLE = false> __device__ __forceinline__ u32x4 chunk_of(const T* row, int k, int d)
 {
     constexpr int V = 16 / (int)sizeof(T);
+    if constexpr (WHOLE) return ((const Chunk*)(row + k))->v;
+    if (k + V <= d) return ((const Chunk*)(row + k))->v;
     T v[V];
-    if (k + V <= d) {
-        load_run<T, V>(row + k, v);
-    } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = k + i < d ? row[k + i] : (T)0.0f;
-    }
+    for (int i = 0; i < V; ++i) v[i] = k + i < d ? row[k + i] : (T)0.0f;
     u32x4 r;
     __builtin_memcpy(&r, v, 16);
     return r;
 }
 
-template <int NT> __device__ __forceinline__ int weight_key(int r) { return (r & 3) | (((r / (4 * NT)) & 1) << 2); }
-
-template <class T, int BM, int BN, int ACT, bool SPLIT>
-__global__ __launch_bounds__(kLinBlock) void k_lin_product(Product p, Epilogue e)
+// where row rho of the weights' operand j stands among a wave's features, and what tells the rows apart that are read together
+template <class T> __device__ __forceinline__ int weight_row(int j, int rho)
 {
+    constexpr int V = 16 / (int)sizeof(T), J = V / 4;
+    return j / J * (4 * V) + (rho >> 2) * V + j % J * 4 + (rho & 3);
+}
+
+template <class T> __device__ __forceinline__ int weight_key(int r) { return (r & 3) | ((r / (16 / (int)sizeof(T))) & 1) << 2; }
+
+// What a lane holds at the end: rows row_of + 16 i, features f0 + 4 V q .. + V.  whole: the workgroup's tile lies inside the output.
+template <class T, int MT, int NT, bool SPLIT>
+__device__ __forceinline__ void lin_epilogue(const f32x4 (&acc)[MT][NT], const Product& p, const Epilogue& e, int64_t row_of, int f0,
+                                             bool whole)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    if (f0 >= p.m) return;
+    float bias[4 * NT];
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) {
+        const int f = f0 + j / V * (4 * V) + j % V;
+        bias[j] = !SPLIT && e.bias && f < p.m ? (float)((const T*)e.bias)[f] : 0.0f;
+    }
+    constexpr int Q = 4 * NT / V, part = MT < 4 ? MT : 4;
+    auto rows = [&](auto all, auto activation) {
+        constexpr bool WHOLE = decltype(all)::value;
+        constexpr int ACT = decltype(activation)::value;
+#pragma unroll
+        for (int i0 = 0; i0 < MT; i0 += part) {
+            // (the residual of four rows at a time, all under way before the first is used: `out` may be the residual itself, so the
+            // compiler may not move a load before a store)
+            u32x4 res[part][Q];
+            if constexpr (!SPLIT) {
+                if (e.residual)
+#pragma unroll
+                    for (int i = 0; i < part; ++i)
+#pragma unroll
+                        for (int q = 0; q < Q; ++q) {
+                            const int64_t row = row_of + (i0 + i) * 16;
+                            const int f = f0 + q * (4 * V);
+                            res[i][q] = WHOLE || (row < p.n && f < p.m) ? chunk_of<T, WHOLE>((const T*)e.residual + row * e.ldr, f, p.m)
+                                                                        : u32x4{0, 0, 0, 0};
+                        }
+            }
+#pragma unroll
+            for (int i = 0; i < part; ++i) {
+                const int64_t row = row_of + (i0 + i) * 16;
+                if (!WHOLE && row >= p.n) continue;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    const int f = f0 + q * (4 * V);
+                    if (!WHOLE && f >= p.m) continue;
+                    const int end = WHOLE ? f + V : p.m;
+                    float z[V];
+#pragma unroll
+                    for (int t = 0; t < V; ++t) z[t] = acc[i0 + i][(q * V + t) / 4][t % 4] + bias[q * V + t];
+                    if constexpr (SPLIT) {
+                        if (f + V <= e.split) {
+                            if (e.out) store_floats<T, V>((T*)e.out + row * e.ldo, f, end, z);
+                        } else if (f >= e.split) {
+                            if (e.out2) store_floats<T, V>((T*)e.out2 + row * e.ldo2, f - e.split, end - e.split, z);
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < V; ++t) {
+                                if (f + t < e.split) {
+                                    if (e.out) ((T*)e.out)[row * e.ldo + f + t] = (T)z[t];
+                                } else if (f + t < p.m && e.out2) {
+                                    ((T*)e.out2)[row * e.ldo2 + f + t - e.split] = (T)z[t];
+                                }
+                            }
+                        }
+                    } else {
+                        if (e.pre) store_floats<T, V>((T*)e.pre + row * e.ldp, f, end, z);
+                        T r[V];
+                        __builtin_memcpy(r, &res[i][q], 16);
+#pragma unroll
+                        for (int t = 0; t < V; ++t) z[t] = act<ACT>(z[t]) + (e.residual ? (float)r[t] : 0.0f);
+                        store_floats<T, V>((T*)e.out + row * e.ldo, f, end, z);
+                    }
+                }
+            }
+        }
+    };
+    if constexpr (SPLIT) {
+        if (whole) rows(std::true_type{}, std::integral_constant<int, GREM_ACT_NONE>{});
+        else rows(std::false_type{}, std::integral_constant<int, GREM_ACT_NONE>{});
+    } else {
+        by_act(e.act, [&](auto activation) {
+            if (whole) rows(std::true_type{}, activation);
+            else rows(std::false_type{}, activation);
+        });
+    }
+}
+
+template <class T, class Tile, bool SPLIT>
+__global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilogue e)
+{
+    constexpr int BM = Tile::BM, BN = Tile::BN;
     constexpr int V = 16 / (int)sizeof(T), K = kLinStep / (int)sizeof(T);
-    constexpr int MT = BM / 32, NT = BN / 32;               // 16 x 16 tiles of a wave: rows, features
-    constexpr int LA = BM / 32, LW = BN / 32;               // chunks a thread stages
+    constexpr int MT = Tile::WM / 16, NT = Tile::WN / 16;   // 16 x 16 tiles of a wave: rows, features
+    constexpr int RS = Tile::threads / 8;                   // rows that the workgroup stages at a time
+    constexpr int LA = BM / RS, LW = BN / RS;               // chunks a thread stages
     __shared__ u32x4 sx[2][BM * 8], sw[2][BN * 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, rho = lane & 15;
-    const int64_t row0 = (int64_t)blockIdx.x * BM;
-    const int col0 = (int)blockIdx.y * BN;
-    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const LinPlace at = lin_place(p.tiles_m);
+    const int64_t row0 = at.row * BM;
+    if (row0 >= p.n) return;
+    const int col0 = at.col * BN;
+    const int wm = wave / (BN / Tile::WN) * Tile::WM, wn = wave % (BN / Tile::WN) * Tile::WN;
     const int sr = threadIdx.x >> 3, sc = threadIdx.x & 7;
     const int steps_a = (p.ka + K - 1) / K, steps = steps_a + (p.kb + K - 1) / K;
 
@@ -126,12 +265,12 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_product(Product p, Epilogue e
     int wrow[LW];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        const int64_t r = row0 + i * 32 + sr;
+        const int64_t r = row0 + i * RS + sr;
         xrow[i] = r < p.n ? r : p.n - 1;
     }
 #pragma unroll
     for (int i = 0; i < LW; ++i) {
-        const int c = col0 + i * 32 + sr;
+        const int c = col0 + i * RS + sr;
         wrow[i] = c < p.m ? c : p.m - 1;
     }
     u32x4 rx[LA], rw[LW];
@@ -141,18 +280,23 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_product(Product p, Epilogue e
         const int64_t ld = first ? p.lda : p.ldb;
         const int k = (first ? step : step - steps_a) * K + sc * V, d = first ? p.ka : p.kb;
         const T* w = (const T*)p.w + (first ? 0 : p.ka);
+        auto all = [&](auto whole) {
+            constexpr bool W = decltype(whole)::value;
 #pragma unroll
-        for (int i = 0; i < LA; ++i) rx[i] = chunk_of<T>(x + xrow[i] * ld, k, d);
+            for (int i = 0; i < LA; ++i) rx[i] = chunk_of<T, W>(x + xrow[i] * ld, k, d);
 #pragma unroll
-        for (int i = 0; i < LW; ++i) rw[i] = chunk_of<T>(w + wrow[i] * p.ldw, k, d);
+            for (int i = 0; i < LW; ++i) rw[i] = chunk_of<T, W>(w + wrow[i] * p.ldw, k, d);
+        };
+        if (k - sc * V + K <= d) all(std::true_type{});
+        else all(std::false_type{});
     };
     auto store = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) sx[buf][(i * 32 + sr) * 8 + (sc ^ (sr & 7))] = rx[i];
+        for (int i = 0; i < LA; ++i) sx[buf][(i * RS + sr) * 8 + (sc ^ (sr & 7))] = rx[i];
 #pragma unroll
         for (int i = 0; i < LW; ++i) {
-            const int r = i * 32 + sr;
-            sw[buf][r * 8 + (sc ^ weight_key<NT>(r))] = rw[i];
+            const int r = i * RS + sr;
+            sw[buf][r * 8 + (sc ^ weight_key<T>(r))] = rw[i];
         }
     };
 
@@ -180,8 +324,8 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_product(Product p, Epilogue e
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const int r = wn + (rho >> 2) * (4 * NT) + j * 4 + (rho & 3);
-                fw[j] = sw[buf][r * 8 + (c ^ weight_key<NT>(r))];
+                const int r = wn + weight_row<T>(j, rho);
+                fw[j] = sw[buf][r * 8 + (c ^ weight_key<T>(r))];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -192,48 +336,135 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_product(Product p, Epilogue e
         __syncthreads();
     }
 
-    // lane (g, rho): row wm + 16 i + rho, features wn + 4 NT g .. + 4 NT
-    const int f0 = col0 + wn + g * (4 * NT);
-    if (f0 >= p.m) return;
-    float bias[4 * NT];
+    lin_epilogue<T, MT, NT, SPLIT>(acc, p, e, row0 + wm + rho, col0 + wn + g * V,
+                                       row0 + BM <= p.n && col0 + BN <= p.m);
+}
+
+// The same product where every run of 16 bytes is whole and aligned: the steps go from memory straight to LDS, and are half as long, so
+// that Tile::stages of them fit and as many less one are under way.  A wave's load instruction fills 16 rows of 64 bytes, in order of its
+// lanes: chunk c of row r lies at c ^ key(r) because the lane at that place asked for chunk c.  Beyond the end of the long
+// axis a lane asks for zeros.
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void mem_void;
+static __device__ __align__(16) const uint32_t lin_zeros[4] = {0, 0, 0, 0};
+
+template <int N> __device__ __forceinline__ void wait_loads_but()
+{
+    static_assert(N < 64, "");
+    // vmcnt = N, and LDS reads all done (a buffer is overwritten after the next barrier)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 0 << 8);
+    asm volatile("" ::: "memory");
+}
+
+template <class T, class Tile, bool SPLIT>
+__global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(2))) void k_lin_direct(Product p, Epilogue e)
+{
+    constexpr int BM = Tile::BM, BN = Tile::BN, S = Tile::stages, H = Tile::halves, waves = Tile::threads / 64;
+    constexpr int V = 16 / (int)sizeof(T), C = 4 * H, K = C * V;       // values of a run; runs and values of a step
+    constexpr int MT = Tile::WM / 16, NT = Tile::WN / 16;
+    constexpr int RW = 64 / C;                                         // rows that a load instruction fills
+    constexpr int LX = BM / RW / waves, LW = BN / RW / waves;          // load instructions of a wave and step
+    __shared__ u32x4 stage[S][(BM + BN) * C];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, rho = lane & 15;
+    const LinPlace at = lin_place(p.tiles_m);
+    const int64_t row0 = at.row * BM;
+    if (row0 >= p.n) return;
+    const int col0 = at.col * BN;
+    const int wm = wave / (BN / Tile::WN) * Tile::WM, wn = wave % (BN / Tile::WN) * Tile::WN;
+    const int steps_a = (p.ka + K - 1) / K, steps = steps_a + (p.kb + K - 1) / K;
+    auto key_x = [](int r) { return H == 2 ? r & 7 : (r >> 1) & 3; };
+    auto key_w = [](int r) { return H == 2 ? weight_key<T>(r) : weight_key<T>(r) >> 1; };
+
+    // a lane's rows, from the block's first one on, and its places in them, in bytes
+    const int rows_here = p.n - row0 < BM ? (int)(p.n - row0) : BM, cols_here = p.m - col0 < BN ? p.m - col0 : BN;
+    int xr[LX], xc[LX], wc[LW];
+    uint32_t xo[LX], wo[LW];
 #pragma unroll
-    for (int j = 0; j < 4 * NT; ++j) bias[j] = !SPLIT && e.bias && f0 + j < p.m ? (float)((const T*)e.bias)[f0 + j] : 0.0f;
+    for (int i = 0; i < LX; ++i) {
+        const int r = (i * waves + wave) * RW + lane / C;
+        xr[i] = r < rows_here ? r : rows_here - 1;
+        xc[i] = ((lane % C) ^ key_x(r)) * V;
+        xo[i] = (uint32_t)((uint32_t)xr[i] * (uint32_t)p.lda + (uint32_t)xc[i]) * (uint32_t)sizeof(T);
+    }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t row = row0 + wm + i * 16 + rho;
-        if (row >= p.n) continue;
+    for (int i = 0; i < LW; ++i) {
+        const int r = (i * waves + wave) * RW + lane / C;
+        wc[i] = ((lane % C) ^ key_w(r)) * V;
+        wo[i] = (uint32_t)((uint32_t)(r < cols_here ? r : cols_here - 1) * (uint32_t)p.ldw + (uint32_t)wc[i]) * (uint32_t)sizeof(T);
+    }
+    const char *x = (const char*)((const T*)p.a + row0 * p.lda), *w = (const char*)((const T*)p.w + (int64_t)col0 * p.ldw);
+    int k = 0, d = p.ka, slot = 0;             // where the next step to load starts, in its source of width d
+    auto load = [&]() {
+        if (k >= d) {                          // on to b
+            x = (const char*)((const T*)p.b + row0 * p.ldb);
+            w = (const char*)((const T*)p.w + (int64_t)col0 * p.ldw + p.ka);
+            k = 0;
+            d = p.kb;
 #pragma unroll
-        for (int q = 0; q < 4 * NT; q += V) {
-            const int f = f0 + q;
-            if (f >= p.m) continue;
-            float z[V];
+            for (int i = 0; i < LX; ++i) xo[i] = (uint32_t)((uint32_t)xr[i] * (uint32_t)p.ldb + (uint32_t)xc[i]) * (uint32_t)sizeof(T);
+        }
+        u32x4* to = stage[slot] + wave * 64;
+        const char *xk = x + (size_t)k * sizeof(T), *wk = w + (size_t)k * sizeof(T);
+        if (k + K <= d) {
 #pragma unroll
-            for (int t = 0; t < V; ++t) z[t] = acc[i][(q + t) / 4][(q + t) % 4] + bias[q + t];
-            if constexpr (SPLIT) {
-                if (f + V <= e.split) {
-                    if (e.out) store_floats<T, V>((T*)e.out + row * e.ldo, f, p.m, z);
-                } else if (f >= e.split) {
-                    if (e.out2) store_floats<T, V>((T*)e.out2 + row * e.ldo2, f - e.split, p.m - e.split, z);
-                } else {
+            for (int i = 0; i < LX; ++i) __builtin_amdgcn_global_load_lds((mem_void*)(xk + xo[i]), (lds_void*)(to + i * waves * 64), 16, 0, 0);
 #pragma unroll
-                    for (int t = 0; t < V; ++t) {
-                        if (f + t < e.split) {
-                            if (e.out) ((T*)e.out)[row * e.ldo + f + t] = (T)z[t];
-                        } else if (f + t < p.m && e.out2) {
-                            ((T*)e.out2)[row * e.ldo2 + f + t - e.split] = (T)z[t];
-                        }
-                    }
-                }
-            } else {
-                if (e.pre) store_floats<T, V>((T*)e.pre + row * e.ldp, f, p.m, z);
-                float r[V];
-                if (e.residual) load_floats<T, V>((const T*)e.residual + row * e.ldr, f, p.m, r);
+            for (int i = 0; i < LW; ++i)
+                __builtin_amdgcn_global_load_lds((mem_void*)(wk + wo[i]), (lds_void*)(to + BM * C + i * waves * 64), 16, 0, 0);
+        } else {
 #pragma unroll
-                for (int t = 0; t < V; ++t) z[t] = act<ACT>(z[t]) + (e.residual ? r[t] : 0.0f);
-                store_floats<T, V>((T*)e.out + row * e.ldo, f, p.m, z);
+            for (int i = 0; i < LX; ++i) {
+                const void* from = k + xc[i] < d ? (const void*)(xk + xo[i]) : (const void*)lin_zeros;
+                __builtin_amdgcn_global_load_lds((mem_void*)from, (lds_void*)(to + i * waves * 64), 16, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < LW; ++i) {
+                const void* from = k + wc[i] < d ? (const void*)(wk + wo[i]) : (const void*)lin_zeros;
+                __builtin_amdgcn_global_load_lds((mem_void*)from, (lds_void*)(to + BM * C + i * waves * 64), 16, 0, 0);
             }
         }
+        k += K;
+        slot = slot + 1 == S ? 0 : slot + 1;
+    };
+
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < S - 1 && s < steps; ++s) load();
+    int now = 0;
+    for (int s = 0; s < steps; ++s) {
+        if (s + S - 2 < steps) wait_loads_but<(S - 2) * (LX + LW)>();
+        else wait_loads_but<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (s + S - 1 < steps) load();
+        const u32x4 *sx = stage[now], *sw = sx + BM * C;
+        now = now + 1 == S ? 0 : now + 1;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            u32x4 fx[MT], fw[NT];
+            const int c = h * 4 + g;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int r = wm + i * 16 + rho;
+                fx[i] = sx[r * C + (c ^ key_x(r))];
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int r = wn + weight_row<T>(j, rho);
+                fw[j] = sw[r * C + (c ^ key_w(r))];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) mma<T>(acc[i][j], fw[j], fx[i]);
+        }
     }
+    lin_epilogue<T, MT, NT, SPLIT>(acc, p, e, row0 + wm + rho, col0 + wn + g * V,
+                                       row0 + BM <= p.n && col0 + BN <= p.m);
 }
 
 // ---- dw = dz^T [a | b] ----------------------------------------------------------------------------------------------------
@@ -247,31 +478,69 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <class T> constexpr int kLinRows = kLinStep / (int)sizeof(T);        // rows of a step
 
-template <class T, bool CK> __device__ __forceinline__ u32x4 source_chunk(const Rows& x, int64_t r, int c, int d)
-{
-    if constexpr (!CK) {
-        return c < d ? chunk_of<T>((const T*)x.data + r * x.stride, c, d) : u32x4{0, 0, 0, 0};
-    } else {
-        constexpr int V = 16 / (int)sizeof(T);
-        float f[V];
-        load_row<T, true, V>(x, r, c, d, f);
+// A run of columns of one row on its way to LDS: 16 bytes of values, or as many codes with their exponent.  The codes are turned into
+// values when they are stored, a step later: the loads stay under way meanwhile.  WHOLE as above.
+template <class T, bool CK> struct Staged {
+    u32x4 v;
+    template <bool WHOLE> __device__ __forceinline__ void load(const Rows& x, int64_t r, int c, int d)
+    {
+        v = WHOLE || c < d ? chunk_of<T, WHOLE>((const T*)x.data + r * x.stride, c, d) : u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ u32x4 values() const { return v; }
+};
+
+template <class T> struct Staged<T, true> {
+    static constexpr int V = 16 / (int)sizeof(T);
+    typedef uint32_t Codes __attribute__((ext_vector_type(V / 4)));
+    struct __attribute__((packed, aligned(1))) Run8 {
+        Codes q;
+    };
+    Codes q;
+    int byte;
+    template <bool WHOLE> __device__ __forceinline__ void load(const Rows& x, int64_t r, int c, int d)
+    {
+        const int8_t* row = (const int8_t*)x.data + r * x.stride;
+        if constexpr (WHOLE) {
+            byte = x.exponents[r * x.exponent_stride + c / kCkGroup];
+            q = ((const Run8*)(row + c))->q;
+            return;
+        }
+        clear();
+        if (c >= d) return;
+        byte = x.exponents[r * x.exponent_stride + c / kCkGroup];
+        int8_t v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = c + i < d ? row[c + i] : (int8_t)0;
+        __builtin_memcpy(&q, v, V);
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) q[i] = 0u;
+        byte = kCkBias;
+    }
+    __device__ __forceinline__ u32x4 values() const
+    {
+        const float scale = ck_scale(byte);
         T v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (T)f[i];
-        u32x4 q;
-        __builtin_memcpy(&q, v, 16);
-        return q;
+        for (int i = 0; i < V; ++i) v[i] = (T)((float)((int32_t)(q[i / 4] << (24 - 8 * (i % 4))) >> 24) * scale);
+        u32x4 out;
+        __builtin_memcpy(&out, v, 16);
+        return out;
     }
-}
+};
 
-template <class T, bool CK, int BM, int BN>
-__global__ __launch_bounds__(kLinBlock) void k_lin_weight(const T* __restrict__ dz, int64_t lddz, Rows a, Rows b, int64_t n, int ka,
-                                                          int kb, int m, int tiles_a, int64_t stretch, float* __restrict__ partial)
+template <class T, bool CK, class Tile>
+__global__ __launch_bounds__(Tile::threads) void k_lin_weight(const T* __restrict__ dz, int64_t lddz, Rows a, Rows b, int64_t n, int ka,
+                                                              int kb, int m, int tiles_a, int64_t stretch, float* __restrict__ partial)
 {
+    constexpr int BM = Tile::BM, BN = Tile::BN, threads = Tile::threads;
     constexpr int V = 16 / (int)sizeof(T), R = kLinRows<T>;
-    constexpr int MT = BM / 32, NT = BN / 32;
-    constexpr int CM = BM / V, CN = BN / V;                          // chunks of a row
-    constexpr int LM = R * CM / kLinBlock, LN = R * CN / kLinBlock;  // chunks a thread stages
+    constexpr int MT = Tile::WM / 16, NT = Tile::WN / 16;
+    constexpr int CM = BM / V, CN = BN / V;                      // chunks of a row
+    constexpr int LM = R * CM / threads, LN = R * CN / threads;  // chunks a thread stages
     // rows are padded by 32 bytes (16 bits) or 64 (floats): the reads of one instruction then cover all banks evenly
     constexpr int PM = CM + (sizeof(T) == 2 ? 2 : 4), PN = CN + (sizeof(T) == 2 ? 2 : 4);
     __shared__ u32x4 sz[2][R * PM], sx[2][R * PN];
@@ -281,40 +550,48 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_weight(const T* __restrict__ 
     const Rows x = first ? a : b;
     const int k0 = (first ? (int)blockIdx.y : (int)blockIdx.y - tiles_a) * BN, kd = first ? ka : kb;
     const int64_t lo = (int64_t)blockIdx.z * stretch, hi = lo + stretch < n ? lo + stretch : n;
-    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const int wm = wave / (BN / Tile::WN) * Tile::WM, wn = wave % (BN / Tile::WN) * Tile::WN;
 
-    u32x4 rz[LM], rx[LN];
+    u32x4 rz[LM];
+    Staged<T, CK> rx[LN];
+    const bool cols_whole = col0 + BM <= m && k0 + BN <= kd;
     auto load = [&](int64_t from) {
+        auto all = [&](auto whole) {
+            constexpr bool W = decltype(whole)::value;
 #pragma unroll
-        for (int i = 0; i < LM; ++i) {
-            const int q = i * kLinBlock + (int)threadIdx.x, r = q / CM, c = col0 + (q % CM) * V;
-            rz[i] = from + r < hi && c < m ? chunk_of<T>(dz + (from + r) * lddz, c, m) : u32x4{0, 0, 0, 0};
-        }
+            for (int i = 0; i < LM; ++i) {
+                const int q = i * threads + (int)threadIdx.x, r = q / CM, c = col0 + (q % CM) * V;
+                rz[i] = W || (from + r < hi && c < m) ? chunk_of<T, W>(dz + (from + r) * lddz, c, m) : u32x4{0, 0, 0, 0};
+            }
 #pragma unroll
-        for (int i = 0; i < LN; ++i) {
-            const int q = i * kLinBlock + (int)threadIdx.x, r = q / CN, c = k0 + (q % CN) * V;
-            rx[i] = from + r < hi ? source_chunk<T, CK>(x, from + r, c, kd) : u32x4{0, 0, 0, 0};
-        }
+            for (int i = 0; i < LN; ++i) {
+                const int q = i * threads + (int)threadIdx.x, r = q / CN, c = k0 + (q % CN) * V;
+                if (W || from + r < hi) rx[i].template load<W>(x, from + r, c, kd);
+                else rx[i].clear();
+            }
+        };
+        if (cols_whole && from + R <= hi) all(std::true_type{});
+        else all(std::false_type{});
     };
     auto store = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < LM; ++i) {
-            const int q = i * kLinBlock + (int)threadIdx.x;
+            const int q = i * threads + (int)threadIdx.x;
             sz[buf][(q / CM) * PM + q % CM] = rz[i];
         }
 #pragma unroll
         for (int i = 0; i < LN; ++i) {
-            const int q = i * kLinBlock + (int)threadIdx.x;
-            sx[buf][(q / CN) * PN + q % CN] = rx[i];
+            const int q = i * threads + (int)threadIdx.x;
+            sx[buf][(q / CN) * PN + q % CN] = rx[i].values();
         }
     };
     // 16 columns from `col` on by half h of the step's rows
     auto operand = [&](const u32x4* s, int pitch, int col, int h) {
         if constexpr (sizeof(T) == 2) {
-            const char* p = (const char*)s + (size_t)(h * 32 + g * 8 + (rho >> 2)) * (size_t)(pitch * 16) + (size_t)(col + (rho & 3) * 4) * 2;
+            const char* p = (const char*)s + (size_t)(h * 32 + g * 4 + (rho >> 2)) * (size_t)(pitch * 16) + (size_t)(col + (rho & 3) * 4) * 2;
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (size_t)(4 * pitch * 16)));
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (size_t)(16 * pitch * 16)));
             u32x4 out;
             __builtin_memcpy(&out, &u, 8);
             __builtin_memcpy((char*)&out + 8, &v, 8);
@@ -463,24 +740,42 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_turn(const T* __restrict__ w,
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
-template <class T, bool SPLIT> void lin_product(const Product& p, const Epilogue& e, int32_t activation, hipStream_t stream)
+constexpr int64_t kLinMostStride = 1 << 23;                  // bytes
+
+template <class T, bool SPLIT> void lin_product(const Product& p, const Epilogue& e, hipStream_t stream)
 {
-    constexpr int BM = 128, BN = 128;
-    const dim3 grid((unsigned)((p.n + BM - 1) / BM), (unsigned)((p.m + BN - 1) / BN));
-    if constexpr (SPLIT)
-        hipLaunchKernelGGL((k_lin_product<T, BM, BN, GREM_ACT_NONE, true>), grid, dim3(kLinBlock), 0, stream, p, e);
-    else
-        by_act(activation, [&](auto a) {
-            hipLaunchKernelGGL((k_lin_product<T, BM, BN, decltype(a)::value, false>), grid, dim3(kLinBlock), 0, stream, p, e);
-        });
+    // where all runs of 16 bytes are whole and aligned, and a block's rows lie within 2^31 bytes: straight to LDS
+    const uint64_t places = (uint64_t)p.a | (uint64_t)p.w | (uint64_t)(p.kb ? p.b : nullptr) |
+                            (uint64_t)((p.lda | p.ldw | p.ka | (p.kb ? p.ldb | p.kb : 0)) * (int64_t)sizeof(T));
+    const int64_t most = kLinMostStride / (int64_t)sizeof(T);
+    const bool direct = places % 16 == 0 && p.lda < most && p.ldw < most && (p.kb == 0 || p.ldb < most);
+    auto run = [&](auto tile) {
+        using Tile = decltype(tile);
+        Product q = p;
+        q.tiles_m = (int)((p.m + Tile::BN - 1) / Tile::BN);
+        const int64_t blocks = (p.n + Tile::BM - 1) / Tile::BM;
+        const dim3 grid((unsigned)((blocks + 7) / 8 * 8 * q.tiles_m));
+        if (direct) hipLaunchKernelGGL((k_lin_direct<T, Tile, SPLIT>), grid, dim3(Tile::threads), 0, stream, q, e);
+        else hipLaunchKernelGGL((k_lin_product<T, Tile, SPLIT>), grid, dim3(Tile::threads), 0, stream, q, e);
+    };
+    // the largest tile of which there are enough for the CUs
+    auto tiles = [&](int64_t t) { return ((p.n + t - 1) / t) * ((p.m + t - 1) / t); };
+    if (p.m > 128 && tiles(256) >= 192) run(LinTile<256, 256, 128, 64, 2, 2>{});
+    else if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64, 2, 2>{});
+    else run(LinTile<64, 64, 32, 32, 2, 2>{});
 }
 
 // the backward pass's workspace
 struct LinSpace {
     int64_t lddz, ldt, stretch;
-    int stretches, parts;
+    int stretches, parts, tile;
     size_t o_dz, o_wt, o_dw, o_bias, bytes;
 };
+
+int lin_weight_tile(int64_t n, int64_t m, int64_t ka, int64_t kb)
+{
+    return n >= 4096 && m > 128 && (ka > 128 || kb > 128) ? 256 : 128;
+}
 
 LinSpace lin_space(int size, int64_t n, int64_t m, int64_t ka, int64_t kb, int32_t activation)
 {
@@ -493,8 +788,10 @@ LinSpace lin_space(int size, int64_t n, int64_t m, int64_t ka, int64_t kb, int32
     s.o_dz = carve(activation == GREM_ACT_NONE ? 0 : (size_t)n * (size_t)s.lddz * size);
     s.o_wt = carve((size_t)(ka + kb) * (size_t)s.ldt * size);
     // stretches of rows: enough workgroups for two a CU, and no shorter than 8 steps
-    const int64_t tiles = ((m + 127) / 128) * ((ka + 127) / 128 + (kb + 127) / 128);
-    int64_t want = tiles ? (512 + tiles - 1) / tiles : 1;
+    s.tile = lin_weight_tile(n, m, ka, kb);
+    const int64_t t = s.tile, tiles = ((m + t - 1) / t) * ((ka + t - 1) / t + (kb + t - 1) / t);
+    const int64_t groups = t == 256 ? 256 : 512;
+    int64_t want = groups / tiles;
     const int64_t most = (n + 8 * rows - 1) / (8 * rows);
     if (want > most) want = most;
     if (want < 1) want = 1;
@@ -531,9 +828,9 @@ extern "C" int grem_linear(int32_t type, int64_t n, int64_t m, const void* a, in
         (pre && !layer_rows_ok(pre, ldp, n, m, size)))
         return GREM_ERR_ARG;
     if (n == 0) return GREM_OK;
-    const Product p{a, b, w, lda, ldb, ldw, n, (int)ka, (int)kb, (int)m};
-    const Epilogue e{bias, residual, out, pre, nullptr, ldr, ldo, ldp, 0, 0};
-    layer_typed(type, [&](auto t) { lin_product<decltype(t), false>(p, e, activation, (hipStream_t)stream); });
+    const Product p{a, b, w, lda, ldb, ldw, n, (int)ka, (int)kb, (int)m, 0};
+    const Epilogue e{bias, residual, out, pre, nullptr, ldr, ldo, ldp, 0, 0, activation};
+    layer_typed(type, [&](auto t) { lin_product<decltype(t), false>(p, e, (hipStream_t)stream); });
     return layer_launched();
 }
 
@@ -587,21 +884,26 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
             T* wt = (T*)(ws + s.o_wt);
             hipLaunchKernelGGL((k_lin_turn<T>), dim3((unsigned)((ka + kb + 31) / 32), (unsigned)((m + 31) / 32)), dim3(kLinBlock), 0, stream,
                                (const T*)w, ldw, (int)m, (int)(ka + kb), wt, s.ldt);
-            const Product p{dz, nullptr, wt, lddz, 0, s.ldt, n, (int)m, 0, (int)(ka + kb)};
-            const Epilogue e{nullptr, nullptr, da, nullptr, db, 0, ldda, 0, lddb, (int)ka};
-            lin_product<T, true>(p, e, GREM_ACT_NONE, stream);
+            const Product p{dz, nullptr, wt, lddz, 0, s.ldt, n, (int)m, 0, (int)(ka + kb), 0};
+            const Epilogue e{nullptr, nullptr, da, nullptr, db, 0, ldda, 0, lddb, (int)ka, GREM_ACT_NONE};
+            lin_product<T, true>(p, e, stream);
         }
         if (dw) {
             float* parts = (float*)(ws + s.o_dw);
-            const int tiles_a = (int)((ka + 127) / 128), tiles_b = (int)((kb + 127) / 128);
-            const dim3 grid((unsigned)((m + 127) / 128), (unsigned)(tiles_a + tiles_b), (unsigned)s.stretches);
             const Rows xa = n ? layer_rows(a) : Rows{}, xb = n && kb ? layer_rows(b) : Rows{};
-            if (n && a->exponents)
-                hipLaunchKernelGGL((k_lin_weight<T, true, 128, 128>), grid, dim3(kLinBlock), 0, stream, dz, lddz, xa, xb, n, (int)ka, (int)kb,
-                                   (int)m, tiles_a, s.stretch, parts);
-            else
-                hipLaunchKernelGGL((k_lin_weight<T, false, 128, 128>), grid, dim3(kLinBlock), 0, stream, dz, lddz, xa, xb, n, (int)ka, (int)kb,
-                                   (int)m, tiles_a, s.stretch, parts);
+            auto weight = [&](auto packed, auto tile) {
+                using Tile = decltype(tile);
+                const int tiles_a = (int)((ka + Tile::BN - 1) / Tile::BN), tiles_b = (int)((kb + Tile::BN - 1) / Tile::BN);
+                hipLaunchKernelGGL((k_lin_weight<T, decltype(packed)::value, Tile>),
+                                   dim3((unsigned)((m + Tile::BM - 1) / Tile::BM), (unsigned)(tiles_a + tiles_b), (unsigned)s.stretches),
+                                   dim3(Tile::threads), 0, stream, dz, lddz, xa, xb, n, (int)ka, (int)kb, (int)m, tiles_a, s.stretch, parts);
+            };
+            auto by_tile = [&](auto packed) {
+                if (s.tile == 256) weight(packed, LinTile<256, 256, 128, 64>{});
+                else weight(packed, LinTile<128, 128, 64, 64>{});
+            };
+            if (n && a->exponents) by_tile(std::integral_constant<bool, true>{});
+            else by_tile(std::integral_constant<bool, false>{});
             const int64_t values = m * (ka + kb), groups = (values + kLinBlock - 1) / kLinBlock;
             hipLaunchKernelGGL((k_lin_join<T>), dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(kLinBlock), 0, stream, parts, s.stretches, values,
                                (int)(ka + kb), (T*)dw, lddw);

@@ -28,9 +28,14 @@ struct NmLong {
 
 template <class T> constexpr int kNmV = 16 / (int)sizeof(T);
 
+__device__ __forceinline__ int64_t nm_start(const void* __restrict__ rowptr, int bits, int64_t v)
+{
+    return bits == 64 ? ((const int64_t*)rowptr)[v] : (int64_t)((const int32_t*)rowptr)[v];
+}
+
 // Adds up the counted entries of [lo, hi) for columns [c0, c0 + L*V*C); every lane ends with the sums of its columns over its own
 // neighbours.  Returns how many entries counted.
-template <class T, class P, bool WEIGHTED, int L, int C>
+template <class T, bool EVEN, bool WEIGHTED, int L, int C>
 __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64_t lo, int64_t hi, const int32_t* __restrict__ labels, int32_t mine,
                                        const int32_t* __restrict__ counts, const T* __restrict__ x, int64_t ldx, int c0, int d,
                                        float (&acc)[C][kNmV<T>])
@@ -57,29 +62,26 @@ __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64
             }
         }
         for (int j = 0; j < kept; j += G * U) {
-            float f[U][C][V], g[U];
+            WordsOf<T, V> f[U][C];
+            float g[U];
 #pragma unroll
             for (int q = 0; q < U; ++q) {
                 const int at = j + q * G + part;
                 const int32_t from = __shfl(u, at & 63);
                 g[q] = WEIGHTED ? __shfl(w, at & 63) : 1.0f;
-                const bool on = at < kept;
+                const int end = at < kept ? d : 0;
 #pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    if (on) {
-                        load_floats<T, V>(x + (int64_t)from * ldx, c + k * L * V, d, f[q][k]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) f[q][k][i] = 0.0f;
-                    }
-                }
+                for (int k = 0; k < C; ++k) f[q][k] = load_words<T, V, EVEN>(x + (int64_t)from * ldx, c + k * L * V, end);
             }
 #pragma unroll
             for (int q = 0; q < U; ++q)
 #pragma unroll
-                for (int k = 0; k < C; ++k)
+                for (int k = 0; k < C; ++k) {
+                    float v[V];
+                    to_floats<T, V>(f[q][k], v);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) acc[k][i] += WEIGHTED ? f[q][k][i] * g[q] : f[q][k][i];
+                    for (int i = 0; i < V; ++i) acc[k][i] += WEIGHTED ? v[i] * g[q] : v[i];
+                }
         }
     }
 #pragma unroll
@@ -91,8 +93,8 @@ __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64
     return total;
 }
 
-template <class T, class P, bool WEIGHTED, int L, int C>
-__global__ __launch_bounds__(kNmBlock) void k_nm_rows(const P* __restrict__ rowptr, const int32_t* __restrict__ colidx, int64_t n,
+template <class T, bool EVEN, bool WEIGHTED, int L, int C>
+__global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ rowptr, int bits, const int32_t* __restrict__ colidx, int64_t n,
                                                       const int32_t* __restrict__ labels, const int32_t* __restrict__ counts,
                                                       const T* __restrict__ x, int64_t ldx, int d, T* __restrict__ out, int64_t ldo,
                                                       int32_t* __restrict__ counts_out, int64_t segment, uint32_t* __restrict__ found,
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const P* __restrict__ rowp
     constexpr int V = kNmV<T>;
     const int lane = threadIdx.x & 63;
     for (int64_t v = (int64_t)blockIdx.x * kNmWaves + (threadIdx.x >> 6); v < n; v += (int64_t)gridDim.x * kNmWaves) {
-        const int64_t lo = (int64_t)rowptr[v], hi = (int64_t)rowptr[v + 1];
+        const int64_t lo = nm_start(rowptr, bits, v), hi = nm_start(rowptr, bits, v + 1);
         const int32_t mine = labels ? labels[v] : 0;
         if (hi - lo > segment && mine >= 0) {
             const int32_t count = (int32_t)((hi - lo + segment - 1) / segment);
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const P* __restrict__ rowp
             for (int k = 0; k < C; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
-            const int total = nm_walk<T, P, WEIGHTED, L, C>(colidx, lo, mine >= 0 ? hi : lo, labels, mine, counts, x, ldx, c0, d, acc);
+            const int total = nm_walk<T, EVEN, WEIGHTED, L, C>(colidx, lo, mine >= 0 ? hi : lo, labels, mine, counts, x, ldx, c0, d, acc);
             if (lane >= L) continue;
             if (c0 == 0 && lane == 0 && counts_out) counts_out[v] = total;
             const float scale = WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1);
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const P* __restrict__ rowp
                 const int c = c0 + (k * L + lane) * V;
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[k][i] *= scale;
-                if (c < d) store_floats<T, V>(out + v * ldo, c, d, acc[k]);
+                if (c < d) store_floats<T, V, EVEN>(out + v * ldo, c, d, acc[k]);
             }
         }
     }
@@ -141,8 +143,8 @@ __global__ void k_nm_clear(uint32_t* __restrict__ found)
 }
 
 // the listed segments, a wave each: sums into partial (a row of d floats an item), counts beside them
-template <class T, class P, bool WEIGHTED, int L, int C>
-__global__ __launch_bounds__(kNmBlock) void k_nm_segments(const P* __restrict__ rowptr, const int32_t* __restrict__ colidx,
+template <class T, bool EVEN, bool WEIGHTED, int L, int C>
+__global__ __launch_bounds__(kNmBlock) void k_nm_segments(const void* __restrict__ rowptr, int bits, const int32_t* __restrict__ colidx,
                                                           const int32_t* __restrict__ labels, const int32_t* __restrict__ counts,
                                                           const T* __restrict__ x, int64_t ldx, int d, int64_t segment,
                                                           const uint32_t* __restrict__ found, const NmItem* __restrict__ items,
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const P* __restrict__ 
     const uint32_t total_items = found[0];
     for (uint32_t it = blockIdx.x * kNmWaves + (threadIdx.x >> 6); it < total_items; it += gridDim.x * kNmWaves) {
         const NmItem item = items[it];
-        const int64_t lo = (int64_t)rowptr[item.row] + item.segment * segment, end = (int64_t)rowptr[item.row + 1];
+        const int64_t lo = nm_start(rowptr, bits, item.row) + item.segment * segment, end = nm_start(rowptr, bits, (int64_t)item.row + 1);
         const int64_t hi = lo + segment < end ? lo + segment : end;
         for (int c0 = 0; c0 < d; c0 += L * V * C) {
             float acc[C][V];
@@ -161,13 +163,13 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const P* __restrict__ 
             for (int k = 0; k < C; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
-            const int total = nm_walk<T, P, WEIGHTED, L, C>(colidx, lo, hi, labels, labels ? labels[item.row] : 0, counts, x, ldx, c0, d, acc);
+            const int total = nm_walk<T, EVEN, WEIGHTED, L, C>(colidx, lo, hi, labels, labels ? labels[item.row] : 0, counts, x, ldx, c0, d, acc);
             if (lane >= L) continue;
             if (c0 == 0 && lane == 0) part_counts[it] = total;
 #pragma unroll
             for (int k = 0; k < C; ++k) {
                 const int c = c0 + (k * L + lane) * V;
-                if (c < d) store_floats<float, V>(partial + (size_t)it * (size_t)d, c, d, acc[k]);
+                if (c < d) store_floats<float, V, EVEN>(partial + (size_t)it * (size_t)d, c, d, acc[k]);
             }
         }
     }
@@ -280,23 +282,17 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
         using T = decltype(t);
         nm_shaped<T>(d, [&](auto shape) {
             constexpr int L = decltype(shape)::L, C = decltype(shape)::C;
-            auto run = [&](auto ptr, auto w) {
-                using P = decltype(ptr);
-                constexpr bool W = decltype(w)::value;
-                hipLaunchKernelGGL((k_nm_rows<T, P, W, L, C>), dim3(grid), dim3(kNmBlock), 0, stream, (const P*)rowptr, colidx, n, labels,
-                                   counts, (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs);
+            auto run = [&](auto even, auto w) {
+                constexpr bool E = decltype(even)::value, W = decltype(w)::value;
+                hipLaunchKernelGGL((k_nm_rows<T, E, W, L, C>), dim3(grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, n, labels, counts,
+                                   (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs);
                 if (!s.items) return;
-                hipLaunchKernelGGL((k_nm_segments<T, P, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, (const P*)rowptr, colidx,
-                                   labels, counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
+                hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
+                                   counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
                 hipLaunchKernelGGL((k_nm_join<T, W>), dim3(join_grid), dim3(kNmBlock), 0, stream, (int)d, found, longs, partial,
                                    part_counts, (T*)out, ldo, counts_out);
             };
-            auto by_weight = [&](auto ptr) {
-                if (weighted) run(ptr, std::integral_constant<bool, true>{});
-                else run(ptr, std::integral_constant<bool, false>{});
-            };
-            if (bits == 64) by_weight(int64_t{});
-            else by_weight(int32_t{});
+            layer_either(d % kNmV<T> == 0, [&](auto even) { layer_either(weighted, [&](auto w) { run(even, w); }); });
         });
     });
     return layer_launched();
