@@ -165,7 +165,7 @@ def load():
     size = ctypes.c_size_t
     rows = ctypes.POINTER(Rows)
     for name, res, args in (
-            ("grem_neighbour_mean_bytes", size, [i64, i64]),
+            ("grem_neighbour_mean_bytes", size, [i32, i64, i64, i64, i32]),
             ("grem_neighbour_mean", ctypes.c_int, [vp, i32, vp, i64, i64, vp, i32, i64, vp, i64, vp, i64, vp, vp, size, vp]),
             ("grem_neighbour_mean_backward", ctypes.c_int,
              [vp, i32, vp, i64, i64, vp, vp, i32, i64, vp, i64, vp, i64, vp, size, vp]),
@@ -548,9 +548,39 @@ def grem_expected_cut_noalloc_max_n() -> int:
 
 # ---- layers on a partitioned graph ------------------------------------------------------------------------------
 
-def _on(stream):
-    """What a call allocates (outputs, workspace) belongs to the stream that it runs on."""
-    return torch.cuda.stream(stream)
+# the current stream's handle without a Stream object around it (2.7 us of a call's 14)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+class _Stream:
+    """The stream of a call.  What the call allocates (outputs, workspace) belongs to the stream that it runs on; the
+    current one is the allocator's own choice, and switching to it would cost a small call a fifth of its time."""
+
+    def __init__(self, stream, device):
+        self.other = stream
+        if stream is None:
+            self.handle = _raw_stream(device.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
+        else:
+            self.handle = stream.cuda_stream
+
+    def empty(self, shape, dtype, device):
+        if self.other is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(self.other):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+    def matrix(self, out, shape, dtype, device, what: str):
+        """`out` checked, or a new matrix; with its pointer and the values between its rows."""
+        if out is None:
+            out = self.empty(shape, dtype, device)
+            return out, out.data_ptr(), shape[1]
+        return (out, *_matrix(out, dtype, shape, what))
+
+    def workspace(self, nbytes: int, device):
+        if nbytes == 0:
+            return None, None, 0
+        buf = self.empty(nbytes, torch.uint8, device)
+        return buf, buf.data_ptr(), nbytes
 
 
 def _type(t: torch.Tensor, what: str) -> int:
@@ -567,14 +597,17 @@ def _matrix(t: torch.Tensor, dtype, shape, what: str):
         raise TypeError(f"{what} must be a tensor on the GPU")
     if t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     n, d = shape
-    if d > 1 and n > 0 and t.stride(1) != 1:
+    between, beside = t.stride()
+    if d > 1 and n > 0 and beside != 1:
         raise ValueError(f"the values of a row of {what} must lie side by side (strides {t.stride()})")
-    if n > 1 and t.stride(0) < d:
+    if n < 2:
+        between = d
+    elif between < d:
         raise ValueError(f"the rows of {what} overlap (strides {t.stride()})")
-    return t.data_ptr(), max(t.stride(0), d) if n > 1 else d
+    return t.data_ptr(), between
 
 
 def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str):
@@ -601,36 +634,21 @@ def _source(t: Union[torch.Tensor, Checkpoint], dtype, shape, what: str) -> Rows
     return Rows(p, ld, e, lde)
 
 
-def _like(out, shape, dtype, device, what: str):
-    """`out` checked, or a new matrix."""
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-    return (out, *_matrix(out, dtype, shape, what))
-
-
-def _workspace(nbytes: int, device) -> tuple:
-    if nbytes == 0:
-        return None, None, 0
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return buf, buf.data_ptr(), nbytes
-
-
 def grem_neighbour_mean(rowptr, colidx, n, x, labels=None, out=None, stream=None):
     """Returns (out (n, d), counts int32[n]): the mean over every vertex's neighbours of its own partition, and how many
     they are; without labels over all neighbours."""
     t = _type(x, "x")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, x.device)
     d = x.shape[1] if x.dim() == 2 else 0
     px, ldx = _matrix(x, x.dtype, (n, d), "x")
     if rowptr.numel() != n + 1:
         raise ValueError(f"rowptr must have {n + 1} entries, got {rowptr.numel()}")
-    with _on(stream):
-        out, po, ldo = _like(out, (n, d), x.dtype, x.device, "out")
-        counts = torch.empty(n, dtype=torch.int32, device=x.device)
-        keep, ws, nbytes = _workspace(lib.grem_neighbour_mean_bytes(colidx.numel(), d), x.device)
-        rc = lib.grem_neighbour_mean(_dev(rowptr, rowptr.dtype, "rowptr"), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel(), n,
-                                     _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo, counts.data_ptr(), ws, nbytes,
-                                     stream.cuda_stream)
+    out, po, ldo = on.matrix(out, (n, d), x.dtype, x.device, "out")
+    counts = on.empty(n, torch.int32, x.device)
+    keep, ws, nbytes = on.workspace(lib.grem_neighbour_mean_bytes(t, n, colidx.numel(), d, labels is not None), x.device)
+    rc = lib.grem_neighbour_mean(_dev(rowptr, rowptr.dtype, "rowptr"), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel(), n,
+                                 _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo, counts.data_ptr(), ws, nbytes,
+                                 on.handle)
     _check(rc, "grem_neighbour_mean")
     return out, counts
 
@@ -638,18 +656,17 @@ def grem_neighbour_mean(rowptr, colidx, n, x, labels=None, out=None, stream=None
 def grem_neighbour_mean_backward(rowptr_t, colidx_t, n, dout, counts, labels=None, dx=None, stream=None) -> torch.Tensor:
     """dx (n, d) from dout and the forward call's counts; rowptr_t, colidx_t: the transposed graph (a symmetric one is its own)."""
     t = _type(dout, "dout")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, dout.device)
     d = dout.shape[1] if dout.dim() == 2 else 0
     pd, ldd = _matrix(dout, dout.dtype, (n, d), "dout")
     if rowptr_t.numel() != n + 1:
         raise ValueError(f"rowptr_t must have {n + 1} entries, got {rowptr_t.numel()}")
-    with _on(stream):
-        dx, px, ldx = _like(dx, (n, d), dout.dtype, dout.device, "dx")
-        keep, ws, nbytes = _workspace(lib.grem_neighbour_mean_bytes(colidx_t.numel(), d), dout.device)
-        rc = lib.grem_neighbour_mean_backward(_dev(rowptr_t, rowptr_t.dtype, "rowptr_t"), _rowptr_bits(rowptr_t), _colidx(colidx_t),
-                                              colidx_t.numel(), n, _vector(labels, torch.int32, n, "labels"),
-                                              _vector(counts, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes,
-                                              stream.cuda_stream)
+    dx, px, ldx = on.matrix(dx, (n, d), dout.dtype, dout.device, "dx")
+    keep, ws, nbytes = on.workspace(lib.grem_neighbour_mean_bytes(t, n, colidx_t.numel(), d, labels is not None), dout.device)
+    rc = lib.grem_neighbour_mean_backward(_dev(rowptr_t, rowptr_t.dtype, "rowptr_t"), _rowptr_bits(rowptr_t), _colidx(colidx_t),
+                                          colidx_t.numel(), n, _vector(labels, torch.int32, n, "labels"),
+                                          _vector(counts, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes,
+                                          on.handle)
     _check(rc, "grem_neighbour_mean_backward")
     return dx
 
@@ -657,7 +674,7 @@ def grem_neighbour_mean_backward(rowptr_t, colidx_t, n, dout, counts, labels=Non
 def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, want_pre=False, stream=None):
     """act([a | b] w^T + bias) + residual, (n, m); with want_pre also z = [a | b] w^T + bias, as (out, z)."""
     t = _type(a, "a")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, a.device)
     if a.dim() != 2 or w.dim() != 2 or (b is not None and b.dim() != 2):
         raise ValueError("a, b and w must be matrices")
     n, ka, kb, m = a.shape[0], a.shape[1], 0 if b is None else b.shape[1], w.shape[0]
@@ -665,11 +682,10 @@ def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, 
     pb, ldb = (None, 0) if b is None else _matrix(b, a.dtype, (n, kb), "b")
     pw, ldw = _matrix(w, a.dtype, (m, ka + kb), "w")
     pr, ldr = (None, 0) if residual is None else _matrix(residual, a.dtype, (n, m), "residual")
-    with _on(stream):
-        out, po, ldo = _like(out, (n, m), a.dtype, a.device, "out")
-        z, pz, ldz = _like(None, (n, m), a.dtype, a.device, "pre") if want_pre else (None, None, 0)
-        rc = lib.grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, a.dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
-                             stream.cuda_stream)
+    out, po, ldo = on.matrix(out, (n, m), a.dtype, a.device, "out")
+    z, pz, ldz = on.matrix(None, (n, m), a.dtype, a.device, "pre") if want_pre else (None, None, 0)
+    rc = lib.grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, a.dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
+                         on.handle)
     _check(rc, "grem_linear")
     return (out, z) if want_pre else out
 
@@ -678,7 +694,7 @@ def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs
     """Returns (da, db, dw, dbias); db is None without b, and so are the inputs' or the parameters' gradients that are not
     wanted.  a, b: the forward call's inputs, or checkpoints of them; pre: its z (not used without an activation)."""
     t = _type(dout, "dout")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, dout.device)
     if dout.dim() != 2 or w.dim() != 2:
         raise ValueError("dout and w must be matrices")
     dtype, dev = dout.dtype, dout.device
@@ -689,15 +705,14 @@ def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs
     if act != ACT_NONE and pre is None:
         raise ValueError("an activation's backward pass needs pre")
     pz, ldz = _matrix(pre, dtype, (n, m), "pre") if act != ACT_NONE else (None, 0)
-    with _on(stream):
-        da, pda, ldda = _like(None, (n, ka), dtype, dev, "da") if want_inputs else (None, None, 0)
-        db, pdb, lddb = _like(None, (n, kb), dtype, dev, "db") if want_inputs and kb else (None, None, 0)
-        dw, pdw, lddw = _like(None, (m, ka + kb), dtype, dev, "dw") if want_params else (None, None, 0)
-        dbias = torch.empty(m, dtype=dtype, device=dev) if want_params else None
-        keep, ws, nbytes = _workspace(lib.grem_linear_backward_bytes(t, n, m, ka, kb, act), dev)
-        rc = lib.grem_linear_backward(t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb), kb,
-                                      pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes,
-                                      stream.cuda_stream)
+    da, pda, ldda = on.matrix(None, (n, ka), dtype, dev, "da") if want_inputs else (None, None, 0)
+    db, pdb, lddb = on.matrix(None, (n, kb), dtype, dev, "db") if want_inputs and kb else (None, None, 0)
+    dw, pdw, lddw = on.matrix(None, (m, ka + kb), dtype, dev, "dw") if want_params else (None, None, 0)
+    dbias = on.empty(m, dtype, dev) if want_params else None
+    keep, ws, nbytes = on.workspace(lib.grem_linear_backward_bytes(t, n, m, ka, kb, act), dev)
+    rc = lib.grem_linear_backward(t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb), kb,
+                                  pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes,
+                                  on.handle)
     _check(rc, "grem_linear_backward")
     return da, db, dw, dbias
 
@@ -705,14 +720,13 @@ def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs
 def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     """Returns (y (n, d), mean float32[n], rstd float32[n])."""
     t = _type(x, "x")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, x.device)
     n, d = x.shape if x.dim() == 2 else (0, 0)
     px, ldx = _matrix(x, x.dtype, (n, d), "x")
-    with _on(stream):
-        out, po, ldo = _like(out, (n, d), x.dtype, x.device, "out")
-        mean, rstd = (torch.empty(n, dtype=torch.float32, device=x.device) for _ in range(2))
-        rc = lib.grem_layer_norm(t, n, d, px, ldx, _vector(gamma, x.dtype, d, "gamma"), _vector(beta, x.dtype, d, "beta"), float(eps), po,
-                                 ldo, mean.data_ptr(), rstd.data_ptr(), stream.cuda_stream)
+    out, po, ldo = on.matrix(out, (n, d), x.dtype, x.device, "out")
+    mean, rstd = (on.empty(n, torch.float32, x.device) for _ in range(2))
+    rc = lib.grem_layer_norm(t, n, d, px, ldx, _vector(gamma, x.dtype, d, "gamma"), _vector(beta, x.dtype, d, "beta"), float(eps), po,
+                             ldo, mean.data_ptr(), rstd.data_ptr(), on.handle)
     _check(rc, "grem_layer_norm")
     return out, mean, rstd
 
@@ -720,18 +734,17 @@ def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
 def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params=True, stream=None):
     """Returns (dx, dgamma, dbeta) (the last two None unless wanted); x: the forward call's input, or a checkpoint of it."""
     t = _type(dy, "dy")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, dy.device)
     n, d = dy.shape if dy.dim() == 2 else (0, 0)
     pd, ldd = _matrix(dy, dy.dtype, (n, d), "dy")
     rx = _source(x, dy.dtype, (n, d), "x")
-    with _on(stream):
-        dx, px, ldx = _like(dx, (n, d), dy.dtype, dy.device, "dx")
-        dgamma, dbeta = (torch.empty(d, dtype=dy.dtype, device=dy.device) if want_params else None for _ in range(2))
-        keep, ws, nbytes = _workspace(lib.grem_layer_norm_backward_bytes(n, d) if want_params else 0, dy.device)
-        rc = lib.grem_layer_norm_backward(t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, torch.float32, n, "mean"),
-                                          _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dy.dtype, d, "gamma"), px, ldx,
-                                          None if dgamma is None else dgamma.data_ptr(), None if dbeta is None else dbeta.data_ptr(),
-                                          ws, nbytes, stream.cuda_stream)
+    dx, px, ldx = on.matrix(dx, (n, d), dy.dtype, dy.device, "dx")
+    dgamma, dbeta = (on.empty(d, dy.dtype, dy.device) if want_params else None for _ in range(2))
+    keep, ws, nbytes = on.workspace(lib.grem_layer_norm_backward_bytes(n, d) if want_params else 0, dy.device)
+    rc = lib.grem_layer_norm_backward(t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, torch.float32, n, "mean"),
+                                      _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dy.dtype, d, "gamma"), px, ldx,
+                                      None if dgamma is None else dgamma.data_ptr(), None if dbeta is None else dbeta.data_ptr(),
+                                      ws, nbytes, on.handle)
     _check(rc, "grem_layer_norm_backward")
     return dx, dgamma, dbeta
 
@@ -739,14 +752,13 @@ def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params
 def grem_checkpoint_pack(x, stream=None) -> Checkpoint:
     """x's rows in 8 bits: groups of 32 columns, int8 codes and one exponent byte each."""
     t = _type(x, "x")
-    lib, stream = load(), stream or torch.cuda.current_stream()
+    lib, on = load(), _Stream(stream, x.device)
     n, d = x.shape if x.dim() == 2 else (0, 0)
     px, ldx = _matrix(x, x.dtype, (n, d), "x")
     groups = -(-d // CHECKPOINT_GROUP)
-    with _on(stream):
-        codes = torch.empty((n, d), dtype=torch.int8, device=x.device)
-        exponents = torch.empty((n, groups), dtype=torch.uint8, device=x.device)
-        rc = lib.grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, stream.cuda_stream)
+    codes = on.empty((n, d), torch.int8, x.device)
+    exponents = on.empty((n, groups), torch.uint8, x.device)
+    rc = lib.grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, on.handle)
     _check(rc, "grem_checkpoint_pack")
     return Checkpoint(codes, exponents, x.dtype)
 
@@ -757,9 +769,8 @@ def grem_checkpoint_unpack(checkpoint: Checkpoint, out=None, stream=None) -> tor
     if checkpoint.dtype not in TYPES:
         raise TypeError(f"a checkpoint is read back as float32, bfloat16 or float16, not {checkpoint.dtype}")
     rx = _source(checkpoint, checkpoint.dtype, (n, d), "checkpoint")
-    lib, stream = load(), stream or torch.cuda.current_stream()
-    with _on(stream):
-        out, po, ldo = _like(out, (n, d), checkpoint.dtype, checkpoint.codes.device, "out")
-        rc = lib.grem_checkpoint_unpack(TYPES[checkpoint.dtype], n, d, ctypes.byref(rx), po, ldo, stream.cuda_stream)
+    lib, on = load(), _Stream(stream, checkpoint.codes.device)
+    out, po, ldo = on.matrix(out, (n, d), checkpoint.dtype, checkpoint.codes.device, "out")
+    rc = lib.grem_checkpoint_unpack(TYPES[checkpoint.dtype], n, d, ctypes.byref(rx), po, ldo, on.handle)
     _check(rc, "grem_checkpoint_unpack")
     return out

@@ -12,7 +12,8 @@
 namespace {
 
 constexpr int kLnBlock = 256;
-constexpr int kLnGroups = 1024;                 // workgroups of the backward pass, at most: each leaves 8d bytes
+constexpr int kLnGroups = 768;                  // workgroups of the backward pass, at most: each leaves 8d bytes (three a CU: 1,024 of them
+                                                // end in a second round that is mostly empty, 301 us for 280 at 262,144 x 1,024)
 
 template <class T> constexpr int kLnV = 16 / (int)sizeof(T);
 
@@ -301,23 +302,15 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_columns_wide(const T* __restric
         }
 }
 
-// The partial rows of `parts` workgroups added up: a workgroup takes 16 of the 2d columns, 16 threads a column, then those in order.
+// partial: rows of d sums for gamma and d for beta
 template <class T>
-__global__ __launch_bounds__(kLnBlock) void k_ln_join(const float* __restrict__ partial, int parts, int d, T* __restrict__ dgamma,
-                                                      T* __restrict__ dbeta)
+__global__ __launch_bounds__(kJoinBlock) void k_ln_join(const float* __restrict__ partial, int parts, int d, T* __restrict__ dgamma,
+                                                        T* __restrict__ dbeta)
 {
-    __shared__ float sums[16][17];
-    const int64_t c = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
-    const int q = threadIdx.x >> 4;
-    float s = 0.0f;
-    if (c < 2 * (int64_t)d)
-        for (int p = q; p < parts; p += 16) s += partial[(size_t)p * 2 * (size_t)d + c];
-    sums[q][threadIdx.x & 15] = s;
-    __syncthreads();
-    if (threadIdx.x >= 16 || c >= 2 * (int64_t)d) return;
-    float total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) total += sums[i][threadIdx.x];
+    __shared__ float sums[kJoinSlices][kJoinCols + 1];
+    const int64_t c = (int64_t)blockIdx.x * kJoinCols + threadIdx.x % kJoinCols;
+    const float total = join_columns(partial, parts, 2 * (int64_t)d, c, sums);
+    if (threadIdx.x >= kJoinCols || c >= 2 * (int64_t)d) return;
     if (c < d) {
         if (dgamma) dgamma[c] = (T)total;
     } else {
@@ -425,7 +418,7 @@ extern "C" int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, cons
                 }
             }
             if (params)
-                hipLaunchKernelGGL((k_ln_join<T>), dim3((unsigned)((2 * d + 15) / 16)), dim3(kLnBlock), 0, stream, partial, parts, (int)d,
+                hipLaunchKernelGGL((k_ln_join<T>), dim3((unsigned)((2 * d + kJoinCols - 1) / kJoinCols)), dim3(kJoinBlock), 0, stream, partial, parts, (int)d,
                                    (T*)dgamma, (T*)dbeta);
         };
         if (n && x->exponents) run(std::integral_constant<bool, true>{});

@@ -667,7 +667,7 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_join(const float* __restrict_
 // (its 256 threads are 32 runs of columns by 8 rows).
 constexpr int kLinDzCols = 32, kLinDzRows = 8;
 
-template <class T, int ACT>
+template <class T, bool EVEN, int ACT>
 __global__ __launch_bounds__(kLinBlock) void k_lin_slope(const T* __restrict__ dout, int64_t ldd, const T* __restrict__ pre, int64_t ldp,
                                                          int64_t n, int m, T* __restrict__ dz, int64_t lddz,
                                                          float* __restrict__ partial)
@@ -682,12 +682,15 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_slope(const T* __restrict__ d
     if (c < m)
         for (int64_t r = (int64_t)blockIdx.x * kLinDzRows + slot; r < n; r += (int64_t)gridDim.x * kLinDzRows) {
             float f[V], z[V];
-            load_floats<T, V>(dout + r * ldd, c, m, f);
+            const WordsOf<T, V> wf = load_words<T, V, EVEN>(dout + r * ldd, c, m);
+            WordsOf<T, V> wz;
+            if constexpr (ACT != GREM_ACT_NONE) wz = load_words<T, V, EVEN>(pre + r * ldp, c, m);
+            to_floats<T, V>(wf, f);
             if constexpr (ACT != GREM_ACT_NONE) {
-                load_floats<T, V>(pre + r * ldp, c, m, z);
+                to_floats<T, V>(wz, z);
 #pragma unroll
                 for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(z[i]);
-                store_floats<T, V>(dz + r * lddz, c, m, f);
+                store_floats<T, V, EVEN>(dz + r * lddz, c, m, f);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += f[i];
@@ -705,22 +708,13 @@ __global__ __launch_bounds__(kLinBlock) void k_lin_slope(const T* __restrict__ d
     }
 }
 
-// dbias: a workgroup takes 16 columns, 16 threads a column, then those in order
 template <class T>
-__global__ __launch_bounds__(kLinBlock) void k_lin_bias(const float* __restrict__ partial, int parts, int m, T* __restrict__ dbias)
+__global__ __launch_bounds__(kJoinBlock) void k_lin_bias(const float* __restrict__ partial, int parts, int m, T* __restrict__ dbias)
 {
-    __shared__ float sums[16][17];
-    const int c = (int)blockIdx.x * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
-    float s = 0.0f;
-    if (c < m)
-        for (int p = q; p < parts; p += 16) s += partial[(size_t)p * (size_t)m + c];
-    sums[q][threadIdx.x & 15] = s;
-    __syncthreads();
-    if (threadIdx.x >= 16 || c >= m) return;
-    float total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) total += sums[i][threadIdx.x];
-    dbias[c] = (T)total;
+    __shared__ float sums[kJoinSlices][kJoinCols + 1];
+    const int64_t c = (int64_t)blockIdx.x * kJoinCols + threadIdx.x % kJoinCols;
+    const float total = join_columns(partial, parts, m, c, sums);
+    if (threadIdx.x < kJoinCols && c < m) dbias[c] = (T)total;
 }
 
 // w (m x width) turned: wt (width x m), so that dz w is a product of the first kind
@@ -760,8 +754,10 @@ template <class T, bool SPLIT> void lin_product(const Product& p, const Epilogue
     };
     // the largest tile of which there are enough for the CUs
     auto tiles = [&](int64_t t) { return ((p.n + t - 1) / t) * ((p.m + t - 1) / t); };
-    if (p.m > 128 && tiles(256) >= 192) run(LinTile<256, 256, 128, 64, 2, 2>{});
-    else if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64, 2, 2>{});
+    // (floats: four times the instructions a step, so that the smaller tile's loads are hidden too)
+    if constexpr (sizeof(T) == 2)
+        if (p.m > 128 && tiles(256) >= 192) return run(LinTile<256, 256, 128, 64, 2, 2>{});
+    if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64, 2, 2>{});
     else run(LinTile<64, 64, 32, 32, 2, 2>{});
 }
 
@@ -801,8 +797,10 @@ LinSpace lin_space(int size, int64_t n, int64_t m, int64_t ka, int64_t kb, int32
     s.stretches = (int)((n + s.stretch - 1) / s.stretch);
     if (s.stretches < 1) s.stretches = 1;
     s.o_dw = carve((size_t)s.stretches * (size_t)m * (size_t)(ka + kb) * 4);
+    // workgroups of the pass that makes dz: about 2,048, over all columns
+    const int64_t across = (m + kLinDzCols * V - 1) / (kLinDzCols * V), down = (2048 + across - 1) / across;
     s.parts = (int)((n + kLinDzRows - 1) / kLinDzRows);
-    if (s.parts > 1024) s.parts = 1024;
+    if (s.parts > down) s.parts = (int)down;
     s.o_bias = carve((size_t)s.parts * (size_t)m * 4);
     s.bytes = off;
     return s;
@@ -869,8 +867,11 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
         if (n && (activation != GREM_ACT_NONE || dbias)) {
             T* made = (T*)(ws + s.o_dz);
             by_act(activation, [&](auto act) {
-                hipLaunchKernelGGL((k_lin_slope<T, decltype(act)::value>), dim3((unsigned)s.parts, (unsigned)((m + kLinDzCols * V - 1) / (kLinDzCols * V))),
-                                   dim3(kLinBlock), 0, stream, (const T*)dout, ldd, (const T*)pre, ldp, n, (int)m, made, s.lddz, bias_parts);
+                layer_either(m % V == 0, [&](auto even) {
+                    hipLaunchKernelGGL((k_lin_slope<T, decltype(even)::value, decltype(act)::value>),
+                                       dim3((unsigned)s.parts, (unsigned)((m + kLinDzCols * V - 1) / (kLinDzCols * V))), dim3(kLinBlock), 0, stream,
+                                       (const T*)dout, ldd, (const T*)pre, ldp, n, (int)m, made, s.lddz, bias_parts);
+                });
             });
             if (activation != GREM_ACT_NONE) {
                 dz = made;
@@ -878,7 +879,7 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
             }
         }
         if (dbias)
-            hipLaunchKernelGGL((k_lin_bias<T>), dim3((unsigned)((m + 15) / 16)), dim3(kLinBlock), 0, stream, bias_parts, n ? s.parts : 0, (int)m,
+            hipLaunchKernelGGL((k_lin_bias<T>), dim3((unsigned)((m + kJoinCols - 1) / kJoinCols)), dim3(kJoinBlock), 0, stream, bias_parts, n ? s.parts : 0, (int)m,
                                (T*)dbias);
         if (n && (da || db)) {
             T* wt = (T*)(ws + s.o_wt);

@@ -4,20 +4,25 @@
 //   dx[u]  = sum over the v that have u in N(v) of dout[v] / |N(v)|: the same walk over the transposed graph with a weight per entry
 //
 // The rows are gathered: an entry costs a row of d values from wherever it lies, and what bounds the kernels is how many such reads are
-// under way and how many of them the caches serve.  A wave takes a vertex.  64 entries at a time it reads columns and labels, moves the
-// entries that count to the front (a permutation of the lanes, so rows of other partitions are never touched), and then L lanes read
-// a neighbour's row, 16 bytes each, 64/L neighbours side by side and four such sets under way.  Sums are held in 32 bits per lane and
-// joined over the wave at the end.
-// Rows of more than `segment` entries go on a list, are summed in segments by as many waves, and joined in order: no atomics on
-// values, the same bytes on every run.
+// under way and how many of them the caches serve.  A wave takes kNmRows vertices: it reads their entries' columns and labels, 256 at
+// a time, and lists those that count in LDS (rows of other partitions are never touched).  Then L lanes read a neighbour's row, 16
+// bytes each, and 64/L such groups take equal stretches of the list, whole rounds of reads under way at once, whichever vertices they
+// belong to; a vertex whose entries lie in two groups' stretches is joined in LDS.  Sums are held in 32 bits.
+// Where a labelling is given and x outgrows the L2s, vertices are taken in order of their partitions (k_nm_histogram, k_nm_order: one
+// counting sort of the labels' low bits), an eighth of them on each chiplet: a partition's rows then meet in one L2.  The look-up of a
+// neighbour's label is as much a read of a cache line as half its row is; from a copy in bytes (labels up to 254) it stays in
+// the L2 too.
+// Rows of more than `segment` entries are taken apart, summed by as many waves, and joined in order: no atomics on values, the
+// same bytes on every run.
 #include "grem_layers.hip.h"
 
 namespace {
 
 constexpr int kNmBlock = 256;
 constexpr int kNmWaves = kNmBlock / 64;
-constexpr int64_t kNmSegment = 512;             // entries a wave takes alone, at least
-constexpr int64_t kNmMostSegments = 65536;      // longer segments rather than more of them
+constexpr int kNmRows = 8;                      // vertices a wave takes at a time
+constexpr int kNmListed = 128;                  // entries of a row that goes on the list: the list holds kNmRows such rows
+constexpr int64_t kNmSegment = 128;             // entries that a long row is cut into, at least
 
 struct NmItem {
     int32_t row, segment;
@@ -26,11 +31,21 @@ struct NmLong {
     int32_t row, first, count, unused;
 };
 
+// found: how many segments and long rows there are; then a histogram of the labels and how much of it has been handed out
+constexpr int kNmBins = 256, kNmWide = 2 + 2 * kNmBins, kNmFound = kNmWide + 1;      // (kNmWide: a label beyond 254 was met)
+constexpr int kNmOrderRows = 4096;              // vertices of a workgroup of the two kernels that order them
+
 template <class T> constexpr int kNmV = 16 / (int)sizeof(T);
 
 __device__ __forceinline__ int64_t nm_start(const void* __restrict__ rowptr, int bits, int64_t v)
 {
     return bits == 64 ? ((const int64_t*)rowptr)[v] : (int64_t)((const int32_t*)rowptr)[v];
+}
+
+__device__ __forceinline__ float nm_weight(const int32_t* __restrict__ counts, int32_t u)
+{
+    const int32_t k = counts[u];
+    return 1.0f / (float)(k > 1 ? k : 1);
 }
 
 // Adds up the counted entries of [lo, hi) for columns [c0, c0 + L*V*C); every lane ends with the sums of its columns over its own
@@ -40,7 +55,7 @@ __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64
                                        const int32_t* __restrict__ counts, const T* __restrict__ x, int64_t ldx, int c0, int d,
                                        float (&acc)[C][kNmV<T>])
 {
-    constexpr int V = kNmV<T>, G = 64 / L, U = 4;
+    constexpr int V = kNmV<T>, G = 64 / L, U = C > 1 ? 4 : 8;
     const int lane = threadIdx.x & 63, part = lane / L, c = c0 + (lane % L) * V;
     int total = 0;
     for (int64_t base = lo; base < hi; base += 64) {
@@ -57,8 +72,7 @@ __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64
         float w = 1.0f;
         if constexpr (WEIGHTED) {
             if (lane < kept) {
-                const int32_t k = counts[u];
-                w = 1.0f / (float)(k > 1 ? k : 1);
+                w = nm_weight(counts, u);
             }
         }
         for (int j = 0; j < kept; j += G * U) {
@@ -93,53 +107,279 @@ __device__ __forceinline__ int nm_walk(const int32_t* __restrict__ colidx, int64
     return total;
 }
 
+// (LDS of one wave: its lanes are in step, only the compiler has to keep the order)
+__device__ __forceinline__ void nm_wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 template <class T, bool EVEN, bool WEIGHTED, int L, int C>
 __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ rowptr, int bits, const int32_t* __restrict__ colidx, int64_t n,
                                                       const int32_t* __restrict__ labels, const int32_t* __restrict__ counts,
                                                       const T* __restrict__ x, int64_t ldx, int d, T* __restrict__ out, int64_t ldo,
                                                       int32_t* __restrict__ counts_out, int64_t segment, uint32_t* __restrict__ found,
-                                                      NmItem* __restrict__ items, NmLong* __restrict__ longs)
+                                                      NmItem* __restrict__ items, NmLong* __restrict__ longs,
+                                                      const int32_t* __restrict__ order, const uint8_t* __restrict__ bytes)
 {
-    constexpr int V = kNmV<T>;
-    const int lane = threadIdx.x & 63;
-    for (int64_t v = (int64_t)blockIdx.x * kNmWaves + (threadIdx.x >> 6); v < n; v += (int64_t)gridDim.x * kNmWaves) {
-        const int64_t lo = nm_start(rowptr, bits, v), hi = nm_start(rowptr, bits, v + 1);
-        const int32_t mine = labels ? labels[v] : 0;
-        if (hi - lo > segment && mine >= 0) {
-            const int32_t count = (int32_t)((hi - lo + segment - 1) / segment);
-            int32_t first = 0;
-            if (lane == 0) {
-                first = (int32_t)atomicAdd(&found[0], (uint32_t)count);
-                longs[atomicAdd(&found[1], 1u)] = NmLong{(int32_t)v, first, count, 0};
-            }
-            first = __shfl(first, 0);
-            for (int32_t i = lane; i < count; i += 64) items[first + i] = NmItem{(int32_t)v, i};
-            continue;
+    constexpr int V = kNmV<T>, G = 64 / L, U = C > 1 ? 4 : 8, R = kNmRows, N = R * kNmListed;
+    __shared__ int32_t list_of[kNmWaves][N];
+    __shared__ float weight_of[WEIGHTED ? kNmWaves : 1][WEIGHTED ? N : 1];
+    __shared__ int32_t off_of[kNmWaves][R + 1], vertex_of[kNmWaves][R];
+    __shared__ float open_of[G > 1 ? kNmWaves : 1][2][G][G > 1 ? L * V * C : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane / L, mine_c = (lane % L) * V;
+    int32_t *list = list_of[wave], *off = off_of[wave], *vertices = vertex_of[wave];
+    float* weights = weight_of[WEIGHTED ? wave : 0];
+    auto& open = open_of[G > 1 ? wave : 0];
+    const bool narrow = bytes && found[kNmWide] == 0u;
+    // the vertices' order cut in eight, one for the workgroups of each chiplet (they go to the chiplets in turn)
+    const int64_t share = order ? (n + 7) / 8 : n, base_at = order ? (int64_t)(blockIdx.x & 7u) * share : 0;
+    const int64_t end_at = base_at + share < n ? base_at + share : n;
+    const int64_t block = order ? blockIdx.x >> 3 : blockIdx.x, blocks = order ? gridDim.x >> 3 : gridDim.x;
+    for (int64_t p0 = base_at + (block * kNmWaves + wave) * R; p0 < end_at; p0 += blocks * kNmWaves * R) {
+        // lane r: row r's vertex, entries, label and what becomes of it
+        const int rows = end_at - p0 < R ? (int)(end_at - p0) : R;
+        const bool is_row = lane < rows;
+        int32_t v = 0, label = 0;
+        int64_t start = 0, degree = 0;
+        if (is_row) {
+            v = order ? order[p0 + lane] : (int32_t)(p0 + lane);
+            start = nm_start(rowptr, bits, v);
+            degree = nm_start(rowptr, bits, (int64_t)v + 1) - start;
+            if (labels) label = labels[v];
         }
+        const bool counted = is_row && label >= 0;
+        const bool cut = counted && degree > segment, walked = counted && !cut && degree > kNmListed;
+        if (cut) {
+            const int32_t count = (int32_t)((degree + segment - 1) / segment);
+            const int32_t first = (int32_t)atomicAdd(&found[0], (uint32_t)count);
+            longs[atomicAdd(&found[1], 1u)] = NmLong{v, first, count, 0};
+            for (int32_t i = 0; i < count; ++i) items[first + i] = NmItem{v, i};
+        }
+
+        // the entries of the rows that go on the list, one row after the other: place q is entry q + from of its row
+        const int32_t length = counted && degree <= kNmListed ? (int32_t)degree : 0;
+        int32_t ends = length;
+#pragma unroll
+        for (int o = 1; o < R; o <<= 1) {
+            const int32_t y = __shfl_up(ends, o);
+            if (lane >= o) ends += y;
+        }
+        const int32_t begins = ends - length, places = __shfl(ends, R - 1);
+        const int64_t from = start - begins;
+        int32_t bound[R];
+#pragma unroll
+        for (int k = 1; k < R; ++k) bound[k] = __shfl(begins, k);
+        // the list, in that order; lane r counts what lies before its row
+        int32_t kept = 0, before = 0;
+        for (int32_t base = 0; base < places; base += 256) {
+            int row[4];
+            int32_t u[4], l[4];
+            bool on[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t at = base + q * 64 + lane;
+                int r = 0;
+#pragma unroll
+                for (int k = 1; k < R; ++k) r += at >= bound[k];
+                row[q] = r;
+                on[q] = at < places;
+                const int64_t shift = __shfl(from, r);
+                u[q] = on[q] ? colidx[shift + at] : 0;
+            }
+            if (labels) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) l[q] = !on[q] ? -1 : narrow ? (int32_t)bytes[u[q]] : labels[u[q]];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int32_t own = __shfl(label, row[q]);
+                    on[q] = on[q] && l[q] == own;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const unsigned long long mask = __ballot(on[q]);
+                const int to = kept + __popcll(mask & ((1ull << lane) - 1ull));
+                if (on[q]) {
+                    list[to] = u[q];
+                    if constexpr (WEIGHTED) weights[to] = nm_weight(counts, u[q]);
+                }
+                const int32_t ahead = begins - (base + q * 64);
+                before += __popcll(mask & (ahead >= 64 ? ~0ull : ahead <= 0 ? 0ull : (1ull << ahead) - 1ull));
+                kept += __popcll(mask);
+            }
+        }
+        if (lane <= R) off[lane] = lane < rows ? before : kept;
+        if (lane < R) vertices[lane] = v;
+        nm_wave_sync();
+        if (counts_out && is_row && !cut && !walked) counts_out[v] = off[lane + 1] - off[lane];
+
         for (int c0 = 0; c0 < d; c0 += L * V * C) {
+            const int c = c0 + mine_c;
+            auto store = [&](int32_t to, float (&acc)[C][V], float scale) {
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    if (c + k * L * V >= d) continue;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[k][i] *= scale;
+                    store_floats<T, V, EVEN>(out + to * ldo, c + k * L * V, d, acc[k]);
+                }
+            };
+            auto scale_of = [&](int r) { return WEIGHTED ? 1.0f : 1.0f / (float)(off[r + 1] - off[r]); };
+            const int stretch = (kept + G - 1) / G;
+            const int j0 = part * stretch < kept ? part * stretch : kept, j1 = j0 + stretch < kept ? j0 + stretch : kept;
+            int r = 0;
+            while (r < R && off[r + 1] <= j0) ++r;
             float acc[C][V];
 #pragma unroll
             for (int k = 0; k < C; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
-            const int total = nm_walk<T, EVEN, WEIGHTED, L, C>(colidx, lo, mine >= 0 ? hi : lo, labels, mine, counts, x, ldx, c0, d, acc);
-            if (lane >= L) continue;
-            if (c0 == 0 && lane == 0 && counts_out) counts_out[v] = total;
-            const float scale = WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1);
+            int end = r < R ? (off[r + 1] < j1 ? off[r + 1] : j1) : j1;
+            for (int j = j0; j < j1; j += U) {
+                WordsOf<T, V> f[U][C];
+                float g[U];
 #pragma unroll
-            for (int k = 0; k < C; ++k) {
-                const int c = c0 + (k * L + lane) * V;
+                for (int q = 0; q < U; ++q) {
+                    const int at = j + q < j1 ? j + q : j1 - 1, width = j + q < j1 ? d : 0;
+                    const int32_t u = list[at];
+                    g[q] = WEIGHTED ? weights[at] : 1.0f;
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[k][i] *= scale;
-                if (c < d) store_floats<T, V, EVEN>(out + v * ldo, c, d, acc[k]);
+                    for (int k = 0; k < C; ++k) f[q][k] = load_words<T, V, EVEN>(x + (int64_t)u * ldx, c + k * L * V, width);
+                }
+#pragma unroll
+                for (int q = 0; q < U; ++q) {
+#pragma unroll
+                    for (int k = 0; k < C; ++k) {
+                        float v[V];
+                        to_floats<T, V>(f[q][k], v);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[k][i] += WEIGHTED ? v[i] * g[q] : v[i];
+                    }
+                    if (j + q + 1 == end) {
+                        // the row's last entry in this stretch
+                        if (G == 1 || (off[r] >= j0 && off[r + 1] <= j1)) {
+                            store(vertices[r], acc, scale_of(r));
+                        } else {
+                            float* to = open[off[r] >= j0 ? 1 : 0][part];
+#pragma unroll
+                            for (int k = 0; k < C; ++k)
+#pragma unroll
+                                for (int i = 0; i < V; ++i) to[k * L * V + mine_c + i] = acc[k][i];
+                        }
+#pragma unroll
+                        for (int k = 0; k < C; ++k)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
+                        while (r < R && off[r + 1] <= end) ++r;
+                        end = r < R && off[r + 1] < j1 ? off[r + 1] : j1;
+                    }
+                }
+            }
+            if constexpr (G > 1) {
+                nm_wave_sync();
+                // a row that starts in this group's stretch and goes on in the next ones
+                if (j0 < j1 && r < R && off[r] >= j0 && off[r] < j1 && off[r + 1] > j1) {
+#pragma unroll
+                    for (int k = 0; k < C; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[k][i] = open[1][part][k * L * V + mine_c + i];
+                    for (int h = part + 1; h < G && h * stretch < off[r + 1]; ++h)
+#pragma unroll
+                        for (int k = 0; k < C; ++k)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) acc[k][i] += open[0][h][k * L * V + mine_c + i];
+                    store(vertices[r], acc, scale_of(r));
+                }
+                nm_wave_sync();
+            }
+            // rows without a counted entry
+            const unsigned long long bare = __ballot(is_row && !cut && !walked && off[lane + 1] == off[lane]);
+#pragma unroll
+            for (int k = 0; k < C; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
+            for (int q = part; q < rows; q += G)
+                if (bare >> q & 1) store(vertices[q], acc, 0.0f);
+            // rows too long for the list, one after the other
+            for (unsigned long long left = __ballot(walked); left; left &= left - 1) {
+                const int q = __ffsll((long long)left) - 1;
+                const int64_t first = __shfl(start, q), last = first + __shfl(degree, q);
+#pragma unroll
+                for (int k = 0; k < C; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
+                const int total = nm_walk<T, EVEN, WEIGHTED, L, C>(colidx, first, last, labels, __shfl(label, q), counts, x, ldx, c0, d, acc);
+                if (c0 == 0 && lane == 0 && counts_out) counts_out[vertices[q]] = total;
+                if (part == 0) store(vertices[q], acc, WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1));
             }
         }
+        nm_wave_sync();
     }
 }
 
 __global__ void k_nm_clear(uint32_t* __restrict__ found)
 {
-    if (threadIdx.x < 2) found[threadIdx.x] = 0u;
+    for (int i = threadIdx.x; i < kNmFound; i += blockDim.x) found[i] = 0u;
+}
+
+__global__ __launch_bounds__(kNmBlock) void k_nm_histogram(const int32_t* __restrict__ labels, int64_t n, uint32_t* __restrict__ found,
+                                                           uint8_t* __restrict__ bytes)
+{
+    __shared__ uint32_t bins[kNmBins];
+    bins[threadIdx.x] = 0u;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * kNmOrderRows, hi = lo + kNmOrderRows < n ? lo + kNmOrderRows : n;
+    bool wide = false;
+    for (int64_t v = lo + threadIdx.x; v < hi; v += kNmBlock) {
+        const int32_t l = labels[v];
+        atomicAdd(&bins[l & (kNmBins - 1)], 1u);
+        bytes[v] = (uint8_t)(l < 0 ? 255 : l);
+        wide |= l > 254;
+    }
+    if (wide) found[kNmWide] = 1u;
+    __syncthreads();
+    if (bins[threadIdx.x]) atomicAdd(&found[2 + threadIdx.x], bins[threadIdx.x]);
+}
+
+// order: the vertices by the low bits of their labels (inside a bin as the workgroups come: no result depends on it)
+__global__ __launch_bounds__(kNmBlock) void k_nm_order(const int32_t* __restrict__ labels, int64_t n, uint32_t* __restrict__ found,
+                                                       int32_t* __restrict__ order)
+{
+    __shared__ uint32_t bins[kNmBins], sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t all = found[2 + threadIdx.x];
+    uint32_t before = all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(before, o);
+        if (lane >= o) before += y;
+    }
+    if (lane == 63) sums[wave] = before;
+    bins[threadIdx.x] = 0u;
+    __syncthreads();
+    before -= all;
+    for (int q = 0; q < wave; ++q) before += sums[q];
+    const int64_t lo = (int64_t)blockIdx.x * kNmOrderRows;
+    constexpr int per = kNmOrderRows / kNmBlock;
+    uint32_t bin[per], rank[per];
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+        const int64_t v = lo + i * kNmBlock + threadIdx.x;
+        bin[i] = v < n ? (uint32_t)labels[v] & (kNmBins - 1) : 0u;
+        rank[i] = v < n ? atomicAdd(&bins[bin[i]], 1u) : 0u;
+    }
+    __syncthreads();
+    const uint32_t mine = bins[threadIdx.x];
+    const uint32_t first = before + (mine ? atomicAdd(&found[2 + kNmBins + threadIdx.x], mine) : 0u);
+    __syncthreads();
+    bins[threadIdx.x] = first;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+        const int64_t v = lo + i * kNmBlock + threadIdx.x;
+        if (v < n) order[bins[bin[i]] + rank[i]] = (int32_t)v;
+    }
 }
 
 // the listed segments, a wave each: sums into partial (a row of d floats an item), counts beside them
@@ -175,8 +415,8 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const void* __restrict
     }
 }
 
-// A long row's segments added up, a workgroup a row: the columns 256/S at a time, S threads a column over every S-th segment, then
-// those S in order.
+// A long row's segments added up, a workgroup a row: up to 32 segments a thread a column, more of them S threads a column over every S-th
+// segment, then those S in order.
 template <class T, bool WEIGHTED>
 __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __restrict__ found, const NmLong* __restrict__ longs,
                                                       const float* __restrict__ partial, const int32_t* __restrict__ part_counts,
@@ -184,26 +424,40 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
 {
     constexpr int S = 8, W = kNmBlock / S;
     __shared__ float sums[S][W];
-    __shared__ int totals[kNmBlock];
+    __shared__ int total_of;
     const int q = threadIdx.x / W, i = threadIdx.x % W;
     const uint32_t rows = found[1];
     for (uint32_t l = blockIdx.x; l < rows; l += gridDim.x) {
         const NmLong r = longs[l];
-        int total = 0;
-        for (int s = threadIdx.x; s < r.count; s += kNmBlock) total += part_counts[r.first + s];
-        totals[threadIdx.x] = total;
-        __syncthreads();
-        for (int o = kNmBlock / 2; o > 0; o >>= 1) {
-            if (threadIdx.x < o) totals[threadIdx.x] += totals[threadIdx.x + o];
-            __syncthreads();
+        if (threadIdx.x < 64) {
+            int total = 0;
+            for (int s = threadIdx.x; s < r.count; s += 64) total += part_counts[r.first + s];
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+            if (threadIdx.x == 0) {
+                total_of = total;
+                if (counts_out) counts_out[r.row] = total;
+            }
         }
-        total = totals[0];
-        if (threadIdx.x == 0 && counts_out) counts_out[r.row] = total;
+        __syncthreads();
+        const int total = total_of;
         const float scale = WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1);
+        const float* rowp = partial + (size_t)r.first * (size_t)d;
+        if (r.count <= 32) {
+            for (int c = threadIdx.x; c < d; c += kNmBlock) {
+                float a = 0.0f;
+#pragma unroll 8
+                for (int s = 0; s < r.count; ++s) a += rowp[(size_t)s * (size_t)d + c];
+                out[(int64_t)r.row * ldo + c] = (T)(a * scale);
+            }
+            __syncthreads();
+            continue;
+        }
         for (int c0 = 0; c0 < d; c0 += W) {
             float a = 0.0f;
             if (c0 + i < d)
-                for (int s = q; s < r.count; s += S) a += partial[(size_t)(r.first + s) * (size_t)d + c0 + i];
+#pragma unroll 8
+                for (int s = q; s < r.count; s += S) a += rowp[(size_t)s * (size_t)d + c0 + i];
             sums[q][i] = a;
             __syncthreads();
             if (q == 0 && c0 + i < d) {
@@ -217,26 +471,36 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
     }
 }
 
+constexpr int64_t kNmOrderedBytes = 32 << 20;
+
 // what a call keeps in its workspace
 struct NmSpace {
     int64_t segment, items;
-    size_t o_items, o_longs, o_counts, o_partial, bytes;
+    bool ordered;
+    size_t o_order, o_bytes, o_items, o_longs, o_counts, o_partial, bytes;
 };
 
-NmSpace nm_space(int64_t nnz, int64_t d)
+// Vertices in order of their partitions: from kNmOrderedBytes of x on
+NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
 {
     NmSpace s;
-    s.segment = (nnz + kNmMostSegments - 1) / kNmMostSegments;
+    // as many segments as leave their sums in half a gigabyte, and no more than 65,536 or so: longer ones rather than more
+    int64_t most = ((int64_t)1 << 26) / d;
+    most = most < 4096 ? 4096 : most > 65536 ? 65536 : most;
+    s.segment = (nnz + most - 1) / most;
     if (s.segment < kNmSegment) s.segment = kNmSegment;
     // a row of e > segment entries has fewer than 2e / segment segments
     s.items = nnz > s.segment ? 2 * (nnz / s.segment) + 1 : 0;
-    size_t off = 256;
+    s.ordered = labelled && n * d * size >= kNmOrderedBytes;
+    size_t off = layer_align(kNmFound * 4);
     auto carve = [&](size_t bytes) { const size_t at = off; off += layer_align(bytes); return at; };
+    s.o_order = carve(s.ordered ? (size_t)n * 4 : 0);
+    s.o_bytes = carve(s.ordered ? (size_t)n : 0);
     s.o_items = carve((size_t)s.items * sizeof(NmItem));
     s.o_longs = carve((size_t)s.items * sizeof(NmLong));
     s.o_counts = carve((size_t)s.items * 4);
     s.o_partial = carve((size_t)s.items * (size_t)d * 4);
-    s.bytes = s.items ? off : 0;
+    s.bytes = s.items || s.ordered ? off : 0;
     return s;
 }
 
@@ -265,7 +529,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
         (nnz && !colidx) || !layer_rows_ok(x, ldx, n, d, size) || !layer_rows_ok(out, ldo, n, d, size) || (weighted && n && !counts))
         return GREM_ERR_ARG;
     if (n == 0) return GREM_OK;
-    const NmSpace s = nm_space(nnz, d);
+    const NmSpace s = nm_space(n, nnz, d, size, labels != nullptr);
     if (s.bytes && (!workspace || workspace_bytes < s.bytes)) return GREM_ERR_NOMEM;
     uint8_t* ws = (uint8_t*)workspace;
     uint32_t* found = (uint32_t*)ws;
@@ -273,11 +537,20 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
     NmLong* longs = s.items ? (NmLong*)(ws + s.o_longs) : nullptr;
     int32_t* part_counts = s.items ? (int32_t*)(ws + s.o_counts) : nullptr;
     float* partial = s.items ? (float*)(ws + s.o_partial) : nullptr;
-    const int64_t groups = (n + kNmWaves - 1) / kNmWaves;
-    const unsigned grid = (unsigned)(groups < (1 << 22) ? groups : 1 << 22);
+    const int64_t groups = (n + kNmWaves * kNmRows - 1) / (kNmWaves * kNmRows);
+    const unsigned grid = (unsigned)(((groups < (1 << 22) ? groups : 1 << 22) + 7) / 8 * 8);
     const unsigned seg_grid = (unsigned)(s.items / kNmWaves + 1 < 2048 ? s.items / kNmWaves + 1 : 2048);
     const unsigned join_grid = (unsigned)(s.items < 1024 ? s.items : 1024);
-    if (s.items) hipLaunchKernelGGL(k_nm_clear, dim3(1), dim3(64), 0, stream, found);
+    if (s.bytes) hipLaunchKernelGGL(k_nm_clear, dim3(1), dim3(kNmBlock), 0, stream, found);
+    int32_t* order = nullptr;
+    uint8_t* bytes = nullptr;
+    if (s.ordered) {
+        const dim3 blocks((unsigned)((n + kNmOrderRows - 1) / kNmOrderRows));
+        order = (int32_t*)(ws + s.o_order);
+        bytes = ws + s.o_bytes;
+        hipLaunchKernelGGL(k_nm_histogram, blocks, dim3(kNmBlock), 0, stream, labels, n, found, bytes);
+        hipLaunchKernelGGL(k_nm_order, blocks, dim3(kNmBlock), 0, stream, labels, n, found, order);
+    }
     layer_typed(type, [&](auto t) {
         using T = decltype(t);
         nm_shaped<T>(d, [&](auto shape) {
@@ -285,7 +558,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
             auto run = [&](auto even, auto w) {
                 constexpr bool E = decltype(even)::value, W = decltype(w)::value;
                 hipLaunchKernelGGL((k_nm_rows<T, E, W, L, C>), dim3(grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, n, labels, counts,
-                                   (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs);
+                                   (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs, order, bytes);
                 if (!s.items) return;
                 hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
                                    counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
@@ -300,9 +573,10 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
 
 }  // namespace
 
-extern "C" size_t grem_neighbour_mean_bytes(int64_t nnz, int64_t d)
+extern "C" size_t grem_neighbour_mean_bytes(int32_t type, int64_t n, int64_t nnz, int64_t d, int32_t labelled)
 {
-    return nnz < 0 || d < 1 || d > kLayerMaxCols ? 0 : nm_space(nnz, d).bytes;
+    const int size = layer_size(type);
+    return !size || n < 0 || n > kLayerMaxRows || nnz < 0 || d < 1 || d > kLayerMaxCols ? 0 : nm_space(n, nnz, d, size, labelled != 0).bytes;
 }
 
 extern "C" int grem_neighbour_mean(const void* rowptr, int32_t rowptr_bits, const int32_t* colidx, int64_t nnz, int64_t n,

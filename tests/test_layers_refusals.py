@@ -46,13 +46,15 @@ def test_neighbour_mean(lib):
     bad = SIZES + [dict(rowptr=None), dict(bits=16), dict(colidx=None), dict(nnz=-1), dict(d=0), dict(d=(1 << 20) + 1), dict(x=None), dict(x=P + 2),
                    dict(type=BF16, x=P + 1), dict(ldx=63), dict(out=None), dict(out=P + 1), dict(ldo=0)]
     _expect(lib.grem_neighbour_mean, order, args, bad)
-    need = lib.grem_neighbour_mean_bytes(100_000, 64)
-    assert need > 0 and lib.grem_neighbour_mean_bytes(100, 64) == 0
+    need = lib.grem_neighbour_mean_bytes(F32, 10, 100_000, 64, 1)
+    assert need > 0 and lib.grem_neighbour_mean_bytes(F32, 10, 100, 64, 1) == 0
     _expect(lib.grem_neighbour_mean, order, args, [dict(nnz=100_000), dict(nnz=100_000, ws=P, bytes=need - 1)], B.ERR_NOMEM)
     assert _call(lib.grem_neighbour_mean, order, args, n=0, rowptr=None, nnz=0, colidx=None, x=None, out=None) == B.OK
     order = "rowptr bits colidx nnz n labels counts type d x ldx out ldo ws bytes stream"
     _expect(lib.grem_neighbour_mean_backward, order, args, bad + [dict(counts=None)])
-    assert lib.grem_neighbour_mean_bytes(-1, 64) == 0 and lib.grem_neighbour_mean_bytes(100_000, 0) == 0
+    assert lib.grem_neighbour_mean_bytes(F32, 10, -1, 64, 0) == 0 and lib.grem_neighbour_mean_bytes(F32, 10, 100_000, 0, 0) == 0
+    # a labelling over more rows than the caches hold: their order is kept in the workspace
+    assert lib.grem_neighbour_mean_bytes(BF16, 1 << 20, 100, 64, 1) > 4 << 20 and lib.grem_neighbour_mean_bytes(BF16, 1 << 20, 100, 64, 0) == 0
 
 
 def test_linear(lib):
