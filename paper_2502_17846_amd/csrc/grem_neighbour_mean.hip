@@ -8,7 +8,7 @@
 // a time, and lists those that count in LDS (rows of other partitions are never touched).  Then L lanes read a neighbour's row, 16
 // bytes each, and 64/L such groups take equal stretches of the list, whole rounds of reads under way at once, whichever vertices they
 // belong to; a vertex whose entries lie in two groups' stretches is joined in LDS.  Sums are held in 32 bits.
-// Where a labelling is given and x outgrows the L2s, vertices are taken in order of their partitions (k_nm_histogram, k_nm_order: one
+// Where a labelling is given and x outgrows the L2s, vertices are taken in order of their partitions (k_nm_histogram, k_nm_scan, k_nm_order: one
 // counting sort of the labels' low bits), an eighth of them on each chiplet: a partition's rows then meet in one L2.  The look-up of a
 // neighbour's label is as much a read of a cache line as half its row is; from a copy in bytes (labels up to 254) it stays in
 // the L2 too.
@@ -31,8 +31,8 @@ struct NmLong {
     int32_t row, first, count, unused;
 };
 
-// found: how many segments and long rows there are; then a histogram of the labels and how much of it has been handed out
-constexpr int kNmBins = 256, kNmWide = 2 + 2 * kNmBins, kNmFound = kNmWide + 1;      // (kNmWide: a label beyond 254 was met)
+// found: how many segments and long rows there are; then a histogram of the labels' low bits
+constexpr int kNmBins = 256, kNmWide = 2 + kNmBins, kNmFound = kNmWide + 1;      // (kNmWide: a label beyond 254 was met)
 constexpr int kNmOrderRows = 4096;              // vertices of a workgroup of the two kernels that order them
 
 template <class T> constexpr int kNmV = 16 / (int)sizeof(T);
@@ -320,66 +320,113 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
 
 __global__ void k_nm_clear(uint32_t* __restrict__ found)
 {
-    for (int i = threadIdx.x; i < kNmFound; i += blockDim.x) found[i] = 0u;
+    if (threadIdx.x < 2) found[threadIdx.x] = 0u;
 }
 
-__global__ __launch_bounds__(kNmBlock) void k_nm_histogram(const int32_t* __restrict__ labels, int64_t n, uint32_t* __restrict__ found,
+// how many of a workgroup's vertices fall into each bin, bin by bin (hist: kNmBins rows of `blocks`; one more row says which workgroups
+// met a label beyond 254), and the labels in bytes
+__global__ __launch_bounds__(kNmBlock) void k_nm_histogram(const int32_t* __restrict__ labels, int64_t n, int blocks, uint32_t* __restrict__ hist,
                                                            uint8_t* __restrict__ bytes)
 {
     __shared__ uint32_t bins[kNmBins];
     bins[threadIdx.x] = 0u;
     __syncthreads();
     const int64_t lo = (int64_t)blockIdx.x * kNmOrderRows, hi = lo + kNmOrderRows < n ? lo + kNmOrderRows : n;
-    bool wide = false;
+    int wide = 0;
     for (int64_t v = lo + threadIdx.x; v < hi; v += kNmBlock) {
         const int32_t l = labels[v];
         atomicAdd(&bins[l & (kNmBins - 1)], 1u);
         bytes[v] = (uint8_t)(l < 0 ? 255 : l);
         wide |= l > 254;
     }
-    if (wide) found[kNmWide] = 1u;
-    __syncthreads();
-    if (bins[threadIdx.x]) atomicAdd(&found[2 + threadIdx.x], bins[threadIdx.x]);
+    wide = __syncthreads_or(wide);
+    hist[(size_t)threadIdx.x * (size_t)blocks + blockIdx.x] = bins[threadIdx.x];
+    if (threadIdx.x == 0) hist[(size_t)kNmBins * (size_t)blocks + blockIdx.x] = wide ? 1u : 0u;
 }
 
-// order: the vertices by the low bits of their labels (inside a bin as the workgroups come: no result depends on it)
-__global__ __launch_bounds__(kNmBlock) void k_nm_order(const int32_t* __restrict__ labels, int64_t n, uint32_t* __restrict__ found,
-                                                       int32_t* __restrict__ order)
+// a workgroup a bin: its counts become the sums of those before; the totals and the flag go to found
+__global__ __launch_bounds__(kNmBlock) void k_nm_scan(uint32_t* __restrict__ hist, int blocks, uint32_t* __restrict__ found)
 {
-    __shared__ uint32_t bins[kNmBins], sums[4];
+    __shared__ uint32_t sums[2][kNmWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bin = blockIdx.x;
+    uint32_t* row = hist + (size_t)bin * (size_t)blocks;
+    uint32_t before = 0u;
+    for (int base = 0, turn = 0; base < blocks; base += kNmBlock, turn ^= 1) {
+        const int at = base + (int)threadIdx.x;
+        const uint32_t mine = at < blocks ? row[at] : 0u;
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t y = __shfl_up(upto, o);
+            if (lane >= o) upto += y;
+        }
+        if (lane == 63) sums[turn][wave] = upto;
+        __syncthreads();
+        uint32_t all = 0u;
+#pragma unroll
+        for (int q = 0; q < kNmWaves; ++q) {
+            if (q < wave) upto += sums[turn][q];
+            all += sums[turn][q];
+        }
+        if (at < blocks) row[at] = before + upto - mine;
+        before += all;
+    }
+    if (threadIdx.x == 0) found[bin < kNmBins ? 2 + bin : kNmWide] = before;
+    if (bin == 0 && threadIdx.x < 2) found[threadIdx.x] = 0u;
+}
+
+// order: the vertices by the low bits of their labels, inside a bin as they come.  Which vertices share a wave decides where a row's sum is
+// cut in two, so the order must be the same on every run: ranks are counted by ballots, a wave a stretch of the workgroup's vertices.
+__global__ __launch_bounds__(kNmBlock) void k_nm_order(const int32_t* __restrict__ labels, int64_t n, int blocks, const uint32_t* __restrict__ found,
+                                                       const uint32_t* __restrict__ hist, int32_t* __restrict__ order)
+{
+    __shared__ uint32_t seen[kNmWaves][kNmBins], sums[kNmWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t all = found[2 + threadIdx.x];
-    uint32_t before = all;
+    uint32_t first = all;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(before, o);
-        if (lane >= o) before += y;
+        const uint32_t y = __shfl_up(first, o);
+        if (lane >= o) first += y;
     }
-    if (lane == 63) sums[wave] = before;
-    bins[threadIdx.x] = 0u;
+    if (lane == 63) sums[wave] = first;
+#pragma unroll
+    for (int q = 0; q < kNmWaves; ++q) seen[q][threadIdx.x] = 0u;
     __syncthreads();
-    before -= all;
-    for (int q = 0; q < wave; ++q) before += sums[q];
-    const int64_t lo = (int64_t)blockIdx.x * kNmOrderRows;
+    first -= all;
+    for (int q = 0; q < wave; ++q) first += sums[q];
+    first += hist[(size_t)threadIdx.x * (size_t)blocks + blockIdx.x];
     constexpr int per = kNmOrderRows / kNmBlock;
+    const int64_t lo = (int64_t)blockIdx.x * kNmOrderRows + wave * (per * 64) + lane;
     uint32_t bin[per], rank[per];
 #pragma unroll
-    for (int i = 0; i < per; ++i) {
-        const int64_t v = lo + i * kNmBlock + threadIdx.x;
-        bin[i] = v < n ? (uint32_t)labels[v] & (kNmBins - 1) : 0u;
-        rank[i] = v < n ? atomicAdd(&bins[bin[i]], 1u) : 0u;
-    }
-    __syncthreads();
-    const uint32_t mine = bins[threadIdx.x];
-    const uint32_t first = before + (mine ? atomicAdd(&found[2 + kNmBins + threadIdx.x], mine) : 0u);
-    __syncthreads();
-    bins[threadIdx.x] = first;
-    __syncthreads();
+    for (int i = 0; i < per; ++i) bin[i] = lo + i * 64 < n ? (uint32_t)labels[lo + i * 64] & (kNmBins - 1) : 0u;
 #pragma unroll
     for (int i = 0; i < per; ++i) {
-        const int64_t v = lo + i * kNmBlock + threadIdx.x;
-        if (v < n) order[bins[bin[i]] + rank[i]] = (int32_t)v;
+        unsigned long long same = __ballot(lo + i * 64 < n);
+#pragma unroll
+        for (int bit = 1; bit < kNmBins; bit <<= 1) {
+            const unsigned long long set = __ballot((bin[i] & bit) != 0u);
+            same &= bin[i] & bit ? set : ~set;
+        }
+        const int below = __popcll(same & ((1ull << lane) - 1ull));
+        const uint32_t had = seen[wave][bin[i]];
+        rank[i] = had + below;
+        nm_wave_sync();
+        if (lo + i * 64 < n && below == 0) seen[wave][bin[i]] = had + __popcll(same);
+        nm_wave_sync();
     }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kNmWaves; ++q) {
+        const uint32_t here = seen[q][threadIdx.x];
+        seen[q][threadIdx.x] = first;
+        first += here;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < per; ++i)
+        if (lo + i * 64 < n) order[seen[wave][bin[i]] + rank[i]] = (int32_t)(lo + i * 64);
 }
 
 // the listed segments, a wave each: sums into partial (a row of d floats an item), counts beside them
@@ -476,8 +523,9 @@ constexpr int64_t kNmOrderedBytes = 32 << 20;
 // what a call keeps in its workspace
 struct NmSpace {
     int64_t segment, items;
+    int blocks;                     // workgroups of the kernels that order the vertices
     bool ordered;
-    size_t o_order, o_bytes, o_items, o_longs, o_counts, o_partial, bytes;
+    size_t o_order, o_bytes, o_hist, o_items, o_longs, o_counts, o_partial, bytes;
 };
 
 // Vertices in order of their partitions: from kNmOrderedBytes of x on
@@ -492,10 +540,12 @@ NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
     // a row of e > segment entries has fewer than 2e / segment segments
     s.items = nnz > s.segment ? 2 * (nnz / s.segment) + 1 : 0;
     s.ordered = labelled && n * d * size >= kNmOrderedBytes;
+    s.blocks = (int)((n + kNmOrderRows - 1) / kNmOrderRows);
     size_t off = layer_align(kNmFound * 4);
     auto carve = [&](size_t bytes) { const size_t at = off; off += layer_align(bytes); return at; };
     s.o_order = carve(s.ordered ? (size_t)n * 4 : 0);
     s.o_bytes = carve(s.ordered ? (size_t)n : 0);
+    s.o_hist = carve(s.ordered ? (size_t)(kNmBins + 1) * (size_t)s.blocks * 4 : 0);
     s.o_items = carve((size_t)s.items * sizeof(NmItem));
     s.o_longs = carve((size_t)s.items * sizeof(NmLong));
     s.o_counts = carve((size_t)s.items * 4);
@@ -541,15 +591,17 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
     const unsigned grid = (unsigned)(((groups < (1 << 22) ? groups : 1 << 22) + 7) / 8 * 8);
     const unsigned seg_grid = (unsigned)(s.items / kNmWaves + 1 < 2048 ? s.items / kNmWaves + 1 : 2048);
     const unsigned join_grid = (unsigned)(s.items < 1024 ? s.items : 1024);
-    if (s.bytes) hipLaunchKernelGGL(k_nm_clear, dim3(1), dim3(kNmBlock), 0, stream, found);
     int32_t* order = nullptr;
     uint8_t* bytes = nullptr;
     if (s.ordered) {
-        const dim3 blocks((unsigned)((n + kNmOrderRows - 1) / kNmOrderRows));
+        uint32_t* hist = (uint32_t*)(ws + s.o_hist);
         order = (int32_t*)(ws + s.o_order);
         bytes = ws + s.o_bytes;
-        hipLaunchKernelGGL(k_nm_histogram, blocks, dim3(kNmBlock), 0, stream, labels, n, found, bytes);
-        hipLaunchKernelGGL(k_nm_order, blocks, dim3(kNmBlock), 0, stream, labels, n, found, order);
+        hipLaunchKernelGGL(k_nm_histogram, dim3((unsigned)s.blocks), dim3(kNmBlock), 0, stream, labels, n, s.blocks, hist, bytes);
+        hipLaunchKernelGGL(k_nm_scan, dim3(kNmBins + 1), dim3(kNmBlock), 0, stream, hist, s.blocks, found);
+        hipLaunchKernelGGL(k_nm_order, dim3((unsigned)s.blocks), dim3(kNmBlock), 0, stream, labels, n, s.blocks, found, hist, order);
+    } else if (s.items) {
+        hipLaunchKernelGGL(k_nm_clear, dim3(1), dim3(64), 0, stream, found);
     }
     layer_typed(type, [&](auto t) {
         using T = decltype(t);

@@ -130,3 +130,36 @@ def test_the_same_bytes_every_time_and_on_another_stream():
     dx2 = B.grem_neighbour_mean_backward(rp, ci, g.n, x, counts, labels, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(dx.view(torch.int16), dx2.view(torch.int16))
+
+
+def _large(n, parts, seed):
+    """A graph whose rows take more than the caches hold, with a label in a hundred missing."""
+    rng = np.random.default_rng(seed)
+    rowptr, colidx = _random(n, 16, seed, np.int64, [(11, 3000), (n - 1, 200)])
+    labels = rng.integers(0, parts, n).astype(np.int32)
+    labels[rng.random(n) < 0.01] = -1
+    return rowptr, colidx, labels
+
+
+@pytest.mark.parametrize("parts", [1, 8, 255, 256, 700])
+def test_vertices_in_order_of_their_partitions(parts):
+    # labels in bytes, labels too large for bytes, more labels than bins
+    n, d = 33_003, 256
+    rowptr, colidx, labels = _large(n, parts, parts)
+    assert B.load().grem_neighbour_mean_bytes(0, n, 100, d, 1) > 4 * n             # the form that orders them
+    _check(rowptr, colidx, labels, _values(n, d, torch.float32, 1), _values(n, d, torch.float32, 2), f"{parts} parts")
+
+
+def test_the_order_is_the_same_every_time():
+    # which rows share a wave decides where a sum is cut in two: 32-bit sums show it
+    n, d = 131_101, 64
+    rowptr, colidx, labels = _large(n, 5, 3)
+    rp, ci, lab = (torch.as_tensor(v).to(DEV) for v in (rowptr, colidx, labels))
+    x = _values(n, d, torch.float32, 8).to(DEV)
+    first, counts = B.grem_neighbour_mean(rp, ci, n, x, lab)
+    back = B.grem_neighbour_mean_backward(rp, ci, n, x, counts, lab)
+    for _ in range(8):
+        out, _ = B.grem_neighbour_mean(rp, ci, n, x, lab)
+        assert torch.equal(out.view(torch.int32), first.view(torch.int32))
+        dx = B.grem_neighbour_mean_backward(rp, ci, n, x, counts, lab)
+        assert torch.equal(dx.view(torch.int32), back.view(torch.int32))
