@@ -552,54 +552,64 @@ def grem_expected_cut_noalloc_max_n() -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-class _Stream:
-    """The stream of a call.  What the call allocates (outputs, workspace) belongs to the stream that it runs on; the
-    current one is the allocator's own choice, and switching to it would cost a small call a fifth of its time."""
-
-    def __init__(self, stream, device):
-        self.other = stream
-        if stream is None:
-            self.handle = _raw_stream(device.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
-        else:
-            self.handle = stream.cuda_stream
-
-    def empty(self, shape, dtype, device):
-        if self.other is None:
-            return torch.empty(shape, dtype=dtype, device=device)
-        with torch.cuda.stream(self.other):
-            return torch.empty(shape, dtype=dtype, device=device)
-
-    def matrix(self, out, shape, dtype, device, what: str):
-        """`out` checked, or a new matrix; with its pointer and the values between its rows."""
-        if out is None:
-            out = self.empty(shape, dtype, device)
-            return out, out.data_ptr(), shape[1]
-        return (out, *_matrix(out, dtype, shape, what))
-
-    def workspace(self, nbytes: int, device):
-        if nbytes == 0:
-            return None, None, 0
-        buf = self.empty(nbytes, torch.uint8, device)
-        return buf, buf.data_ptr(), nbytes
+def _handle(stream, like: torch.Tensor):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(like.device.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
 
 
-def _type(t: torch.Tensor, what: str) -> int:
+def _new(stream, like: torch.Tensor, shape, dtype=None) -> torch.Tensor:
+    """What a call allocates (outputs, workspace) belongs to the stream that it runs on; the current one is the allocator's own
+    choice, and switching to it would cost a small call a fifth of its time."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return like.new_empty(shape, dtype=dtype)
+    return like.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _into(stream, out: Optional[torch.Tensor], like: torch.Tensor, n: int, d: int, what: str):
+    """`out` checked, or a new matrix of `like`'s type; with its pointer and the values between its rows."""
+    if out is None:
+        out = _new(stream, like, (n, d))
+        return out, out.data_ptr(), d
+    return (out, *_matrix(out, like.dtype, n, d, what))
+
+
+def _space(stream, like: torch.Tensor, nbytes: int):
+    """A workspace and its pointer."""
+    if nbytes == 0:
+        return None, None
+    buf = _new(stream, like, nbytes, torch.uint8)
+    return buf, buf.data_ptr()
+
+
+def _first(t: torch.Tensor, what: str):
+    """(type, rows, columns) of the matrix whose type is the call's."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
     if t.dtype not in TYPES:
         raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
-    return TYPES[t.dtype]
+    n, d = _sides(t, what)
+    return TYPES[t.dtype], n, d
 
 
-def _matrix(t: torch.Tensor, dtype, shape, what: str):
+def _sides(t: torch.Tensor, what: str):
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be a matrix, got shape {tuple(shape)}")
+    return shape
+
+
+def _matrix(t: torch.Tensor, dtype, n: int, d: int, what: str):
     """(pointer, values between rows) of a matrix whose rows' values lie side by side; rows may be any distance apart."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
     if t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    n, d = shape
+    if t.shape != (n, d):
+        raise ValueError(f"{what} must have shape {(n, d)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), d
     between, beside = t.stride()
     if d > 1 and n > 0 and beside != 1:
         raise ValueError(f"the values of a row of {what} must lie side by side (strides {t.stride()})")
@@ -618,74 +628,79 @@ def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str):
     return _dev(t, dtype, what)
 
 
-def _width(t: Union[torch.Tensor, Checkpoint]) -> int:
-    return (t.codes if isinstance(t, Checkpoint) else t).shape[1]
+def _width(t: Union[torch.Tensor, Checkpoint], what: str) -> int:
+    return _sides(t.codes if isinstance(t, Checkpoint) else t, what)[1]
 
 
-def _source(t: Union[torch.Tensor, Checkpoint], dtype, shape, what: str) -> Rows:
+def _source(t: Union[torch.Tensor, Checkpoint], dtype, n: int, d: int, what: str) -> Rows:
     """grem_rows of a matrix or of a checkpoint of that shape and type."""
     if not isinstance(t, Checkpoint):
-        p, ld = _matrix(t, dtype, shape, what)
+        p, ld = _matrix(t, dtype, n, d, what)
         return Rows(p, ld, None, 0)
     if t.dtype != dtype:
         raise TypeError(f"{what} is a checkpoint of {t.dtype}, not of {dtype}")
-    p, ld = _matrix(t.codes, torch.int8, shape, what + ".codes")
-    e, lde = _matrix(t.exponents, torch.uint8, (shape[0], -(-shape[1] // CHECKPOINT_GROUP)), what + ".exponents")
+    p, ld = _matrix(t.codes, torch.int8, n, d, what + ".codes")
+    e, lde = _matrix(t.exponents, torch.uint8, n, -(-d // CHECKPOINT_GROUP), what + ".exponents")
     return Rows(p, ld, e, lde)
+
+
+def _graph(rowptr: torch.Tensor, colidx: torch.Tensor, n: int, what: str):
+    """(rowptr's pointer, its bits, colidx's pointer, its length)"""
+    if rowptr.numel() != n + 1:
+        raise ValueError(f"{what} must have {n + 1} entries, got {rowptr.numel()}")
+    return _dev(rowptr, rowptr.dtype, what), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel()
 
 
 def grem_neighbour_mean(rowptr, colidx, n, x, labels=None, out=None, stream=None):
     """Returns (out (n, d), counts int32[n]): the mean over every vertex's neighbours of its own partition, and how many
     they are; without labels over all neighbours."""
-    t = _type(x, "x")
-    lib, on = load(), _Stream(stream, x.device)
-    d = x.shape[1] if x.dim() == 2 else 0
-    px, ldx = _matrix(x, x.dtype, (n, d), "x")
-    if rowptr.numel() != n + 1:
-        raise ValueError(f"rowptr must have {n + 1} entries, got {rowptr.numel()}")
-    out, po, ldo = on.matrix(out, (n, d), x.dtype, x.device, "out")
-    counts = on.empty(n, torch.int32, x.device)
-    keep, ws, nbytes = on.workspace(lib.grem_neighbour_mean_bytes(t, n, colidx.numel(), d, labels is not None), x.device)
-    rc = lib.grem_neighbour_mean(_dev(rowptr, rowptr.dtype, "rowptr"), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel(), n,
-                                 _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo, counts.data_ptr(), ws, nbytes,
-                                 on.handle)
+    t, _, d = _first(x, "x")
+    lib = load()
+    px, ldx = _matrix(x, x.dtype, n, d, "x")
+    rp, bits, ci, nnz = _graph(rowptr, colidx, n, "rowptr")
+    out, po, ldo = _into(stream, out, x, n, d, "out")
+    counts = _new(stream, x, n, torch.int32)
+    nbytes = lib.grem_neighbour_mean_bytes(t, n, nnz, d, labels is not None)
+    keep, ws = _space(stream, x, nbytes)
+    rc = lib.grem_neighbour_mean(rp, bits, ci, nnz, n, _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo,
+                                 counts.data_ptr(), ws, nbytes, _handle(stream, x))
     _check(rc, "grem_neighbour_mean")
     return out, counts
 
 
 def grem_neighbour_mean_backward(rowptr_t, colidx_t, n, dout, counts, labels=None, dx=None, stream=None) -> torch.Tensor:
     """dx (n, d) from dout and the forward call's counts; rowptr_t, colidx_t: the transposed graph (a symmetric one is its own)."""
-    t = _type(dout, "dout")
-    lib, on = load(), _Stream(stream, dout.device)
-    d = dout.shape[1] if dout.dim() == 2 else 0
-    pd, ldd = _matrix(dout, dout.dtype, (n, d), "dout")
-    if rowptr_t.numel() != n + 1:
-        raise ValueError(f"rowptr_t must have {n + 1} entries, got {rowptr_t.numel()}")
-    dx, px, ldx = on.matrix(dx, (n, d), dout.dtype, dout.device, "dx")
-    keep, ws, nbytes = on.workspace(lib.grem_neighbour_mean_bytes(t, n, colidx_t.numel(), d, labels is not None), dout.device)
-    rc = lib.grem_neighbour_mean_backward(_dev(rowptr_t, rowptr_t.dtype, "rowptr_t"), _rowptr_bits(rowptr_t), _colidx(colidx_t),
-                                          colidx_t.numel(), n, _vector(labels, torch.int32, n, "labels"),
+    t, _, d = _first(dout, "dout")
+    lib = load()
+    pd, ldd = _matrix(dout, dout.dtype, n, d, "dout")
+    rp, bits, ci, nnz = _graph(rowptr_t, colidx_t, n, "rowptr_t")
+    dx, px, ldx = _into(stream, dx, dout, n, d, "dx")
+    nbytes = lib.grem_neighbour_mean_bytes(t, n, nnz, d, labels is not None)
+    keep, ws = _space(stream, dout, nbytes)
+    rc = lib.grem_neighbour_mean_backward(rp, bits, ci, nnz, n, _vector(labels, torch.int32, n, "labels"),
                                           _vector(counts, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes,
-                                          on.handle)
+                                          _handle(stream, dout))
     _check(rc, "grem_neighbour_mean_backward")
     return dx
 
 
 def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, want_pre=False, stream=None):
     """act([a | b] w^T + bias) + residual, (n, m); with want_pre also z = [a | b] w^T + bias, as (out, z)."""
-    t = _type(a, "a")
-    lib, on = load(), _Stream(stream, a.device)
-    if a.dim() != 2 or w.dim() != 2 or (b is not None and b.dim() != 2):
-        raise ValueError("a, b and w must be matrices")
-    n, ka, kb, m = a.shape[0], a.shape[1], 0 if b is None else b.shape[1], w.shape[0]
-    pa, lda = _matrix(a, a.dtype, (n, ka), "a")
-    pb, ldb = (None, 0) if b is None else _matrix(b, a.dtype, (n, kb), "b")
-    pw, ldw = _matrix(w, a.dtype, (m, ka + kb), "w")
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, a.dtype, (n, m), "residual")
-    out, po, ldo = on.matrix(out, (n, m), a.dtype, a.device, "out")
-    z, pz, ldz = on.matrix(None, (n, m), a.dtype, a.device, "pre") if want_pre else (None, None, 0)
-    rc = lib.grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, a.dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
-                         on.handle)
+    t, n, ka = _first(a, "a")
+    dtype, m, kb = a.dtype, _sides(w, "w")[0], 0
+    pb, ldb, pr, ldr, z, pz, ldz = None, 0, None, 0, None, None, 0
+    pa, lda = _matrix(a, dtype, n, ka, "a")
+    if b is not None:
+        kb = _sides(b, "b")[1]
+        pb, ldb = _matrix(b, dtype, n, kb, "b")
+    pw, ldw = _matrix(w, dtype, m, ka + kb, "w")
+    if residual is not None:
+        pr, ldr = _matrix(residual, dtype, n, m, "residual")
+    out, po, ldo = _into(stream, out, a, n, m, "out")
+    if want_pre:
+        z, pz, ldz = _into(stream, None, a, n, m, "pre")
+    rc = load().grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
+                            _handle(stream, a))
     _check(rc, "grem_linear")
     return (out, z) if want_pre else out
 
@@ -693,84 +708,88 @@ def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, 
 def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs=True, want_params=True, stream=None):
     """Returns (da, db, dw, dbias); db is None without b, and so are the inputs' or the parameters' gradients that are not
     wanted.  a, b: the forward call's inputs, or checkpoints of them; pre: its z (not used without an activation)."""
-    t = _type(dout, "dout")
-    lib, on = load(), _Stream(stream, dout.device)
-    if dout.dim() != 2 or w.dim() != 2:
-        raise ValueError("dout and w must be matrices")
-    dtype, dev = dout.dtype, dout.device
-    n, m, ka, kb = dout.shape[0], dout.shape[1], _width(a), 0 if b is None else _width(b)
-    pd, ldd = _matrix(dout, dtype, (n, m), "dout")
-    pw, ldw = _matrix(w, dtype, (m, ka + kb), "w")
-    ra, rb = _source(a, dtype, (n, ka), "a"), None if b is None else _source(b, dtype, (n, kb), "b")
-    if act != ACT_NONE and pre is None:
-        raise ValueError("an activation's backward pass needs pre")
-    pz, ldz = _matrix(pre, dtype, (n, m), "pre") if act != ACT_NONE else (None, 0)
-    da, pda, ldda = on.matrix(None, (n, ka), dtype, dev, "da") if want_inputs else (None, None, 0)
-    db, pdb, lddb = on.matrix(None, (n, kb), dtype, dev, "db") if want_inputs and kb else (None, None, 0)
-    dw, pdw, lddw = on.matrix(None, (m, ka + kb), dtype, dev, "dw") if want_params else (None, None, 0)
-    dbias = on.empty(m, dtype, dev) if want_params else None
-    keep, ws, nbytes = on.workspace(lib.grem_linear_backward_bytes(t, n, m, ka, kb, act), dev)
+    t, n, m = _first(dout, "dout")
+    dtype, lib = dout.dtype, load()
+    _sides(w, "w")
+    ka, kb = _width(a, "a"), 0 if b is None else _width(b, "b")
+    pd, ldd = _matrix(dout, dtype, n, m, "dout")
+    pw, ldw = _matrix(w, dtype, m, ka + kb, "w")
+    ra, rb = _source(a, dtype, n, ka, "a"), None if b is None else _source(b, dtype, n, kb, "b")
+    pz, ldz = None, 0
+    if act != ACT_NONE:
+        if pre is None:
+            raise ValueError("an activation's backward pass needs pre")
+        pz, ldz = _matrix(pre, dtype, n, m, "pre")
+    da, pda, ldda = _into(stream, None, dout, n, ka, "da") if want_inputs else (None, None, 0)
+    db, pdb, lddb = _into(stream, None, dout, n, kb, "db") if want_inputs and kb else (None, None, 0)
+    dw, pdw, lddw = _into(stream, None, dout, m, ka + kb, "dw") if want_params else (None, None, 0)
+    dbias = _new(stream, dout, m) if want_params else None
+    nbytes = lib.grem_linear_backward_bytes(t, n, m, ka, kb, act)
+    keep, ws = _space(stream, dout, nbytes)
     rc = lib.grem_linear_backward(t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb), kb,
                                   pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes,
-                                  on.handle)
+                                  _handle(stream, dout))
     _check(rc, "grem_linear_backward")
     return da, db, dw, dbias
 
 
 def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     """Returns (y (n, d), mean float32[n], rstd float32[n])."""
-    t = _type(x, "x")
-    lib, on = load(), _Stream(stream, x.device)
-    n, d = x.shape if x.dim() == 2 else (0, 0)
-    px, ldx = _matrix(x, x.dtype, (n, d), "x")
-    out, po, ldo = on.matrix(out, (n, d), x.dtype, x.device, "out")
-    mean, rstd = (on.empty(n, torch.float32, x.device) for _ in range(2))
-    rc = lib.grem_layer_norm(t, n, d, px, ldx, _vector(gamma, x.dtype, d, "gamma"), _vector(beta, x.dtype, d, "beta"), float(eps), po,
-                             ldo, mean.data_ptr(), rstd.data_ptr(), on.handle)
+    t, n, d = _first(x, "x")
+    dtype = x.dtype
+    px, ldx = _matrix(x, dtype, n, d, "x")
+    out, po, ldo = _into(stream, out, x, n, d, "out")
+    mean, rstd = _new(stream, x, n, torch.float32), _new(stream, x, n, torch.float32)
+    rc = load().grem_layer_norm(t, n, d, px, ldx, _vector(gamma, dtype, d, "gamma"), _vector(beta, dtype, d, "beta"), eps, po, ldo,
+                                mean.data_ptr(), rstd.data_ptr(), _handle(stream, x))
     _check(rc, "grem_layer_norm")
     return out, mean, rstd
 
 
 def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params=True, stream=None):
     """Returns (dx, dgamma, dbeta) (the last two None unless wanted); x: the forward call's input, or a checkpoint of it."""
-    t = _type(dy, "dy")
-    lib, on = load(), _Stream(stream, dy.device)
-    n, d = dy.shape if dy.dim() == 2 else (0, 0)
-    pd, ldd = _matrix(dy, dy.dtype, (n, d), "dy")
-    rx = _source(x, dy.dtype, (n, d), "x")
-    dx, px, ldx = on.matrix(dx, (n, d), dy.dtype, dy.device, "dx")
-    dgamma, dbeta = (on.empty(d, dy.dtype, dy.device) if want_params else None for _ in range(2))
-    keep, ws, nbytes = on.workspace(lib.grem_layer_norm_backward_bytes(n, d) if want_params else 0, dy.device)
+    t, n, d = _first(dy, "dy")
+    dtype, lib = dy.dtype, load()
+    pd, ldd = _matrix(dy, dtype, n, d, "dy")
+    rx = _source(x, dtype, n, d, "x")
+    dx, px, ldx = _into(stream, dx, dy, n, d, "dx")
+    dgamma = dbeta = pg = pb = keep = ws = None
+    nbytes = 0
+    if want_params:
+        dgamma, dbeta = _new(stream, dy, d), _new(stream, dy, d)
+        pg, pb = dgamma.data_ptr(), dbeta.data_ptr()
+        nbytes = lib.grem_layer_norm_backward_bytes(n, d)
+        keep, ws = _space(stream, dy, nbytes)
     rc = lib.grem_layer_norm_backward(t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, torch.float32, n, "mean"),
-                                      _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dy.dtype, d, "gamma"), px, ldx,
-                                      None if dgamma is None else dgamma.data_ptr(), None if dbeta is None else dbeta.data_ptr(),
-                                      ws, nbytes, on.handle)
+                                      _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dtype, d, "gamma"), px, ldx, pg, pb,
+                                      ws, nbytes, _handle(stream, dy))
     _check(rc, "grem_layer_norm_backward")
     return dx, dgamma, dbeta
 
 
 def grem_checkpoint_pack(x, stream=None) -> Checkpoint:
     """x's rows in 8 bits: groups of 32 columns, int8 codes and one exponent byte each."""
-    t = _type(x, "x")
-    lib, on = load(), _Stream(stream, x.device)
-    n, d = x.shape if x.dim() == 2 else (0, 0)
-    px, ldx = _matrix(x, x.dtype, (n, d), "x")
+    t, n, d = _first(x, "x")
+    px, ldx = _matrix(x, x.dtype, n, d, "x")
     groups = -(-d // CHECKPOINT_GROUP)
-    codes = on.empty((n, d), torch.int8, x.device)
-    exponents = on.empty((n, groups), torch.uint8, x.device)
-    rc = lib.grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, on.handle)
+    codes, exponents = _new(stream, x, (n, d), torch.int8), _new(stream, x, (n, groups), torch.uint8)
+    rc = load().grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, _handle(stream, x))
     _check(rc, "grem_checkpoint_pack")
     return Checkpoint(codes, exponents, x.dtype)
 
 
 def grem_checkpoint_unpack(checkpoint: Checkpoint, out=None, stream=None) -> torch.Tensor:
     """The values that a checkpoint's codes stand for, in its type."""
-    n, d = checkpoint.codes.shape
-    if checkpoint.dtype not in TYPES:
-        raise TypeError(f"a checkpoint is read back as float32, bfloat16 or float16, not {checkpoint.dtype}")
-    rx = _source(checkpoint, checkpoint.dtype, (n, d), "checkpoint")
-    lib, on = load(), _Stream(stream, checkpoint.codes.device)
-    out, po, ldo = on.matrix(out, (n, d), checkpoint.dtype, checkpoint.codes.device, "out")
-    rc = lib.grem_checkpoint_unpack(TYPES[checkpoint.dtype], n, d, ctypes.byref(rx), po, ldo, on.handle)
+    codes, exponents, dtype = checkpoint
+    n, d = _sides(codes, "checkpoint.codes")
+    if dtype not in TYPES:
+        raise TypeError(f"a checkpoint is read back as float32, bfloat16 or float16, not {dtype}")
+    rx = _source(checkpoint, dtype, n, d, "checkpoint")
+    if out is None:
+        out = _new(stream, codes, (n, d), dtype)
+        po, ldo = out.data_ptr(), d
+    else:
+        po, ldo = _matrix(out, dtype, n, d, "out")
+    rc = load().grem_checkpoint_unpack(TYPES[dtype], n, d, ctypes.byref(rx), po, ldo, _handle(stream, codes))
     _check(rc, "grem_checkpoint_unpack")
     return out

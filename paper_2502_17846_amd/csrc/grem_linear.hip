@@ -649,88 +649,112 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_weight(const T* __restric
     }
 }
 
-// dw[f][c] = sum over the stretches, in order
-template <class T>
-__global__ __launch_bounds__(kLinBlock) void k_lin_join(const float* __restrict__ partial, int stretches, int64_t values, int width,
-                                                        T* __restrict__ dw, int64_t lddw)
-{
-    for (int64_t i = (int64_t)blockIdx.x * kLinBlock + threadIdx.x; i < values; i += (int64_t)gridDim.x * kLinBlock) {
-        float s = 0.0f;
-        for (int q = 0; q < stretches; ++q) s += partial[(int64_t)q * values + i];
-        dw[i / width * lddw + i % width] = (T)s;
-    }
-}
-
 // ---- dz and dbias ---------------------------------------------------------------------------------------------------------
 //
 // One pass over dout and z: dz rounded to its type, and the columns' sums of the unrounded dz, a partial row per workgroup
 // (its 256 threads are 32 runs of columns by 8 rows).
 constexpr int kLinDzCols = 32, kLinDzRows = 8;
 
-template <class T, bool EVEN, int ACT>
-__global__ __launch_bounds__(kLinBlock) void k_lin_slope(const T* __restrict__ dout, int64_t ldd, const T* __restrict__ pre, int64_t ldp,
-                                                         int64_t n, int m, T* __restrict__ dz, int64_t lddz,
-                                                         float* __restrict__ partial)
+template <class T> struct Slope {
+    const T *dout, *pre;
+    T* dz;
+    int64_t ldd, ldp, lddz, n;
+    float* partial;                 // or NULL
+    int m, parts, across;           // workgroups over the rows, over the columns
+};
+
+template <class T, bool EVEN, int ACT> __device__ __forceinline__ void lin_slope(const Slope<T>& p, int part, int piece)
 {
     constexpr int V = 16 / (int)sizeof(T);
     __shared__ float sums[kLinDzRows][kLinDzCols * V + 1];
-    const int col = threadIdx.x % kLinDzCols, slot = threadIdx.x / kLinDzCols;
-    const int c = ((int)blockIdx.y * kLinDzCols + col) * V;
+    const int col = threadIdx.x % kLinDzCols, slot = threadIdx.x / kLinDzCols, m = p.m;
+    const int c = (piece * kLinDzCols + col) * V;
     float s[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = 0.0f;
     if (c < m)
-        for (int64_t r = (int64_t)blockIdx.x * kLinDzRows + slot; r < n; r += (int64_t)gridDim.x * kLinDzRows) {
+        for (int64_t r = (int64_t)part * kLinDzRows + slot; r < p.n; r += (int64_t)p.parts * kLinDzRows) {
             float f[V], z[V];
-            const WordsOf<T, V> wf = load_words<T, V, EVEN>(dout + r * ldd, c, m);
+            const WordsOf<T, V> wf = load_words<T, V, EVEN>(p.dout + r * p.ldd, c, m);
             WordsOf<T, V> wz;
-            if constexpr (ACT != GREM_ACT_NONE) wz = load_words<T, V, EVEN>(pre + r * ldp, c, m);
+            if constexpr (ACT != GREM_ACT_NONE) wz = load_words<T, V, EVEN>(p.pre + r * p.ldp, c, m);
             to_floats<T, V>(wf, f);
             if constexpr (ACT != GREM_ACT_NONE) {
                 to_floats<T, V>(wz, z);
 #pragma unroll
                 for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(z[i]);
-                store_floats<T, V, EVEN>(dz + r * lddz, c, m, f);
+                store_floats<T, V, EVEN>(p.dz + r * p.lddz, c, m, f);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += f[i];
         }
-    if (!partial) return;
+    if (!p.partial) return;
 #pragma unroll
     for (int i = 0; i < V; ++i) sums[slot][col * V + i] = s[i];
     __syncthreads();
     for (int i = threadIdx.x; i < kLinDzCols * V; i += kLinBlock) {
-        const int at = (int)blockIdx.y * kLinDzCols * V + i;
+        const int at = piece * kLinDzCols * V + i;
         float t = 0.0f;
 #pragma unroll
         for (int q = 0; q < kLinDzRows; ++q) t += sums[q][i];
-        if (at < m) partial[(size_t)blockIdx.x * (size_t)m + at] = t;
+        if (at < m) p.partial[(size_t)part * (size_t)m + at] = t;
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kJoinBlock) void k_lin_bias(const float* __restrict__ partial, int parts, int m, T* __restrict__ dbias)
-{
-    __shared__ float sums[kJoinSlices][kJoinCols + 1];
-    const int64_t c = (int64_t)blockIdx.x * kJoinCols + threadIdx.x % kJoinCols;
-    const float total = join_columns(partial, parts, m, c, sums);
-    if (threadIdx.x < kJoinCols && c < m) dbias[c] = (T)total;
-}
-
 // w (m x width) turned: wt (width x m), so that dz w is a product of the first kind
-template <class T>
-__global__ __launch_bounds__(kLinBlock) void k_lin_turn(const T* __restrict__ w, int64_t ldw, int m, int width, T* __restrict__ wt, int64_t ldt)
+template <class T> struct Turn {
+    const T* w;
+    T* wt;
+    int64_t ldw, ldt;
+    int m, width, across;           // tiles of 32 along the width
+};
+
+template <class T> __device__ __forceinline__ void lin_turn(const Turn<T>& p, uint32_t piece)
 {
     __shared__ T tile[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int c0 = (int)blockIdx.x * 32, f0 = (int)blockIdx.y * 32;
+    const int c0 = (int)(piece % (uint32_t)p.across) * 32, f0 = (int)(piece / (uint32_t)p.across) * 32;
 #pragma unroll
     for (int i = 0; i < 32; i += 8)
-        if (f0 + y + i < m && c0 + x < width) tile[y + i][x] = w[(int64_t)(f0 + y + i) * ldw + c0 + x];
+        if (f0 + y + i < p.m && c0 + x < p.width) tile[y + i][x] = p.w[(int64_t)(f0 + y + i) * p.ldw + c0 + x];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 32; i += 8)
-        if (c0 + y + i < width && f0 + x < m) wt[(int64_t)(c0 + y + i) * ldt + f0 + x] = tile[x][y + i];
+        if (c0 + y + i < p.width && f0 + x < p.m) p.wt[(int64_t)(c0 + y + i) * p.ldt + f0 + x] = tile[x][y + i];
+}
+
+// What the products wait for, in one launch: the turned weights' workgroups first, dz's after them.
+template <class T, bool EVEN, int ACT>
+__global__ __launch_bounds__(kLinBlock) void k_lin_prepare(Slope<T> slope, Turn<T> turn, uint32_t turns)
+{
+    if (blockIdx.x < turns) {
+        lin_turn<T>(turn, blockIdx.x);
+    } else {
+        const uint32_t at = blockIdx.x - turns;
+        lin_slope<T, EVEN, ACT>(slope, (int)(at / (uint32_t)slope.across), (int)(at % (uint32_t)slope.across));
+    }
+}
+
+// The partial sums of both parameters, added up in order: dbias by the first workgroups, 16 columns each, dw[f][c] = the sum over the
+// stretches by the others.
+template <class T>
+__global__ __launch_bounds__(kJoinBlock) void k_lin_join(const float* __restrict__ bias_parts, int parts, int m, T* __restrict__ dbias, uint32_t biases,
+                                                         const float* __restrict__ partial, int stretches, int64_t values, int width,
+                                                         T* __restrict__ dw, int64_t lddw)
+{
+    if (blockIdx.x < biases) {
+        __shared__ float sums[kJoinSlices][kJoinCols + 1];
+        const int64_t c = (int64_t)blockIdx.x * kJoinCols + threadIdx.x % kJoinCols;
+        const float total = join_columns(bias_parts, parts, m, c, sums);
+        if (threadIdx.x < kJoinCols && c < m) dbias[c] = (T)total;
+        return;
+    }
+    for (int64_t i = (int64_t)(blockIdx.x - biases) * kJoinBlock + threadIdx.x; i < values; i += (int64_t)(gridDim.x - biases) * kJoinBlock) {
+        float s = 0.0f;
+#pragma unroll 4
+        for (int q = 0; q < stretches; ++q) s += partial[(int64_t)q * values + i];
+        dw[i / width * lddw + i % width] = (T)s;
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -864,13 +888,20 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
         const T* dz = (const T*)dout;
         int64_t lddz = ldd;
         float* bias_parts = dbias ? (float*)(ws + s.o_bias) : nullptr;
-        if (n && (activation != GREM_ACT_NONE || dbias)) {
+        float* parts = (float*)(ws + s.o_dw);
+        T* wt = (T*)(ws + s.o_wt);
+        const bool slopes = n && (activation != GREM_ACT_NONE || dbias), turned = n && (da || db);
+        if (slopes || turned) {
             T* made = (T*)(ws + s.o_dz);
+            const int across = (int)((m + kLinDzCols * V - 1) / (kLinDzCols * V)), tiles = (int)((ka + kb + 31) / 32);
+            const Slope<T> slope{(const T*)dout, (const T*)pre, made, ldd, ldp, s.lddz, n, bias_parts, (int)m, s.parts, across};
+            const Turn<T> turn{(const T*)w, wt, ldw, s.ldt, (int)m, (int)(ka + kb), tiles};
+            const uint32_t turns = turned ? (uint32_t)tiles * (uint32_t)((m + 31) / 32) : 0u;
+            const uint32_t grid = turns + (slopes ? (uint32_t)s.parts * (uint32_t)across : 0u);
             by_act(activation, [&](auto act) {
                 layer_either(m % V == 0, [&](auto even) {
-                    hipLaunchKernelGGL((k_lin_slope<T, decltype(even)::value, decltype(act)::value>),
-                                       dim3((unsigned)s.parts, (unsigned)((m + kLinDzCols * V - 1) / (kLinDzCols * V))), dim3(kLinBlock), 0, stream,
-                                       (const T*)dout, ldd, (const T*)pre, ldp, n, (int)m, made, s.lddz, bias_parts);
+                    hipLaunchKernelGGL((k_lin_prepare<T, decltype(even)::value, decltype(act)::value>), dim3(grid), dim3(kLinBlock), 0, stream, slope,
+                                       turn, turns);
                 });
             });
             if (activation != GREM_ACT_NONE) {
@@ -878,19 +909,12 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
                 lddz = s.lddz;
             }
         }
-        if (dbias)
-            hipLaunchKernelGGL((k_lin_bias<T>), dim3((unsigned)((m + kJoinCols - 1) / kJoinCols)), dim3(kJoinBlock), 0, stream, bias_parts, n ? s.parts : 0, (int)m,
-                               (T*)dbias);
-        if (n && (da || db)) {
-            T* wt = (T*)(ws + s.o_wt);
-            hipLaunchKernelGGL((k_lin_turn<T>), dim3((unsigned)((ka + kb + 31) / 32), (unsigned)((m + 31) / 32)), dim3(kLinBlock), 0, stream,
-                               (const T*)w, ldw, (int)m, (int)(ka + kb), wt, s.ldt);
+        if (turned) {
             const Product p{dz, nullptr, wt, lddz, 0, s.ldt, n, (int)m, 0, (int)(ka + kb), 0};
             const Epilogue e{nullptr, nullptr, da, nullptr, db, 0, ldda, 0, lddb, (int)ka, GREM_ACT_NONE};
             lin_product<T, true>(p, e, stream);
         }
         if (dw) {
-            float* parts = (float*)(ws + s.o_dw);
             const Rows xa = n ? layer_rows(a) : Rows{}, xb = n && kb ? layer_rows(b) : Rows{};
             auto weight = [&](auto packed, auto tile) {
                 using Tile = decltype(tile);
@@ -905,9 +929,12 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
             };
             if (n && a->exponents) by_tile(std::integral_constant<bool, true>{});
             else by_tile(std::integral_constant<bool, false>{});
-            const int64_t values = m * (ka + kb), groups = (values + kLinBlock - 1) / kLinBlock;
-            hipLaunchKernelGGL((k_lin_join<T>), dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(kLinBlock), 0, stream, parts, s.stretches, values,
-                               (int)(ka + kb), (T*)dw, lddw);
+        }
+        if (dw || dbias) {
+            const uint32_t biases = dbias ? (uint32_t)((m + kJoinCols - 1) / kJoinCols) : 0u;
+            const int64_t values = dw ? m * (ka + kb) : 0, groups = (values + kJoinBlock - 1) / kJoinBlock;
+            hipLaunchKernelGGL((k_lin_join<T>), dim3(biases + (unsigned)(groups < 2048 ? groups : 2048)), dim3(kJoinBlock), 0, stream, bias_parts,
+                               n ? s.parts : 0, (int)m, (T*)dbias, biases, parts, s.stretches, values, (int)(ka + kb), (T*)dw, lddw);
         }
     });
     return layer_launched();

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                                                       const T* __restrict__ x, int64_t ldx, int d, T* __restrict__ out, int64_t ldo,
                                                       int32_t* __restrict__ counts_out, int64_t segment, uint32_t* __restrict__ found,
                                                       NmItem* __restrict__ items, NmLong* __restrict__ longs,
-                                                      const int32_t* __restrict__ order, const uint8_t* __restrict__ bytes)
+                                                      const int32_t* __restrict__ order, const uint8_t* __restrict__ bytes, int take)
 {
     constexpr int V = kNmV<T>, G = 64 / L, U = C > 1 ? 4 : 8, R = kNmRows, N = R * kNmListed;
     __shared__ int32_t list_of[kNmWaves][N];
@@ -136,9 +136,9 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
     const int64_t share = order ? (n + 7) / 8 : n, base_at = order ? (int64_t)(blockIdx.x & 7u) * share : 0;
     const int64_t end_at = base_at + share < n ? base_at + share : n;
     const int64_t block = order ? blockIdx.x >> 3 : blockIdx.x, blocks = order ? gridDim.x >> 3 : gridDim.x;
-    for (int64_t p0 = base_at + (block * kNmWaves + wave) * R; p0 < end_at; p0 += blocks * kNmWaves * R) {
+    for (int64_t p0 = base_at + (block * kNmWaves + wave) * take; p0 < end_at; p0 += blocks * kNmWaves * take) {
         // lane r: row r's vertex, entries, label and what becomes of it
-        const int rows = end_at - p0 < R ? (int)(end_at - p0) : R;
+        const int rows = end_at - p0 < take ? (int)(end_at - p0) : take;
         const bool is_row = lane < rows;
         int32_t v = 0, label = 0;
         int64_t start = 0, degree = 0;
@@ -554,6 +554,14 @@ NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
     return s;
 }
 
+// Vertices a wave takes: kNmRows where that still leaves every CU its 16 waves, fewer on smaller graphs.
+int nm_take(int64_t n)
+{
+    int take = kNmRows;
+    while (take > 1 && n < (int64_t)take * 4096) take /= 2;
+    return take;
+}
+
 struct NmL8 { static constexpr int L = 8, C = 1; };
 struct NmL16 { static constexpr int L = 16, C = 1; };
 struct NmL32 { static constexpr int L = 32, C = 1; };
@@ -587,10 +595,11 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
     NmLong* longs = s.items ? (NmLong*)(ws + s.o_longs) : nullptr;
     int32_t* part_counts = s.items ? (int32_t*)(ws + s.o_counts) : nullptr;
     float* partial = s.items ? (float*)(ws + s.o_partial) : nullptr;
-    const int64_t groups = (n + kNmWaves * kNmRows - 1) / (kNmWaves * kNmRows);
+    const int take = nm_take(n);
+    const int64_t groups = (n + kNmWaves * take - 1) / (kNmWaves * take);
     const unsigned grid = (unsigned)(((groups < (1 << 22) ? groups : 1 << 22) + 7) / 8 * 8);
     const unsigned seg_grid = (unsigned)(s.items / kNmWaves + 1 < 2048 ? s.items / kNmWaves + 1 : 2048);
-    const unsigned join_grid = (unsigned)(s.items < 1024 ? s.items : 1024);
+    const unsigned join_grid = (unsigned)(s.items < 4096 ? s.items : 4096);
     int32_t* order = nullptr;
     uint8_t* bytes = nullptr;
     if (s.ordered) {
@@ -610,7 +619,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
             auto run = [&](auto even, auto w) {
                 constexpr bool E = decltype(even)::value, W = decltype(w)::value;
                 hipLaunchKernelGGL((k_nm_rows<T, E, W, L, C>), dim3(grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, n, labels, counts,
-                                   (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs, order, bytes);
+                                   (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs, order, bytes, take);
                 if (!s.items) return;
                 hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
                                    counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
