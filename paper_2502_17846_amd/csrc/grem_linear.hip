@@ -113,8 +113,9 @@ constexpr int kLinBlock = 256;
 constexpr int kLinStep = 128;       // bytes
 
 // BM rows (of the output's n, or features of dz) by BN, of which a wave takes WM by WN
-template <int BM_, int BN_, int WM_, int WN_, int STAGES = 2, int HALVES = 2> struct LinTile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, stages = STAGES, halves = HALVES, threads = BM / WM * (BN / WN) * 64;
+template <int BM_, int BN_, int WM_, int WN_> struct LinTile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, stages = 2, threads = BM / WM * (BN / WN) * 64;
+    static constexpr int lds = stages * (BM + BN) * kLinStep, per_cu = 160 * 1024 / lds, waves_per_simd = per_cu * threads / 256;
 };
 
 // Workgroups go to the eight chiplets in turn.  Those that share a block of rows are given numbers eight apart, so that they run on
@@ -124,9 +125,9 @@ struct LinPlace {
     int col;
 };
 
-__device__ __forceinline__ LinPlace lin_place(int cols)
+__device__ __forceinline__ LinPlace lin_place(uint32_t id, int cols)
 {
-    const uint32_t id = blockIdx.x, chiplet = id & 7u, local = id >> 3;
+    const uint32_t chiplet = id & 7u, local = id >> 3;
     return LinPlace{(int64_t)(local / (uint32_t)cols) * 8 + chiplet, (int)(local % (uint32_t)cols)};
 }
 
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
     constexpr int LA = BM / RS, LW = BN / RS;               // chunks a thread stages
     __shared__ u32x4 sx[2][BM * 8], sw[2][BN * 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, rho = lane & 15;
-    const LinPlace at = lin_place(p.tiles_m);
+    const LinPlace at = lin_place(blockIdx.x, p.tiles_m);
     const int64_t row0 = at.row * BM;
     if (row0 >= p.n) return;
     const int col0 = at.col * BN;
@@ -340,10 +341,14 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
                                        row0 + BM <= p.n && col0 + BN <= p.m);
 }
 
-// The same product where every run of 16 bytes is whole and aligned: the steps go from memory straight to LDS, and are half as long, so
-// that Tile::stages of them fit and as many less one are under way.  A wave's load instruction fills 16 rows of 64 bytes, in order of its
-// lanes: chunk c of row r lies at c ^ key(r) because the lane at that place asked for chunk c.  Beyond the end of the long
-// axis a lane asks for zeros.
+// The same product where every run of 16 bytes is whole and aligned: the steps go from memory straight to LDS, two steps ahead of the
+// products.  A wave's load instruction fills 8 rows of 128 bytes, in order of its lanes: chunk c of row r lies at c ^ key(r) because the lane
+// at that place asked for chunk c.  Beyond the end of the long axis a lane asks for zeros.
+//
+// What bounds it is that path: 65,536 x 2,048 by 1,024 takes 208 us without the loads and 223 without the products, and took 286 with a step's
+// loads sent at once, because a wave that sends them stands until the memory pipeline has taken them all; dealt out between the
+// products 264 (1,040 TFLOP/s).  Four or five steps of 64 bytes under way are slower than two of 128 (338 and 348 us for 300).
+// A workgroup takes tiles one after the other, and the next one's first steps come while one is stored.
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void mem_void;
 static __device__ __align__(16) const uint32_t lin_zeros[4] = {0, 0, 0, 0};
@@ -358,113 +363,152 @@ template <int N> __device__ __forceinline__ void wait_loads_but()
 }
 
 template <class T, class Tile, bool SPLIT>
-__global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(2))) void k_lin_direct(Product p, Epilogue e)
+__global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(Tile::waves_per_simd))) void k_lin_direct(Product p, Epilogue e, uint32_t total)
 {
-    constexpr int BM = Tile::BM, BN = Tile::BN, S = Tile::stages, H = Tile::halves, waves = Tile::threads / 64;
-    constexpr int V = 16 / (int)sizeof(T), C = 4 * H, K = C * V;       // values of a run; runs and values of a step
+    constexpr int BM = Tile::BM, BN = Tile::BN, S = Tile::stages, waves = Tile::threads / 64;
+    constexpr int V = 16 / (int)sizeof(T), C = kLinStep / 16, K = C * V;   // values of a run; runs and values of a step
     constexpr int MT = Tile::WM / 16, NT = Tile::WN / 16;
     constexpr int RW = 64 / C;                                         // rows that a load instruction fills
     constexpr int LX = BM / RW / waves, LW = BN / RW / waves;          // load instructions of a wave and step
     __shared__ u32x4 stage[S][(BM + BN) * C];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, rho = lane & 15;
-    const LinPlace at = lin_place(p.tiles_m);
-    const int64_t row0 = at.row * BM;
-    if (row0 >= p.n) return;
-    const int col0 = at.col * BN;
     const int wm = wave / (BN / Tile::WN) * Tile::WM, wn = wave % (BN / Tile::WN) * Tile::WN;
-    const int steps_a = (p.ka + K - 1) / K, steps = steps_a + (p.kb + K - 1) / K;
-    auto key_x = [](int r) { return H == 2 ? r & 7 : (r >> 1) & 3; };
-    auto key_w = [](int r) { return H == 2 ? weight_key<T>(r) : weight_key<T>(r) >> 1; };
+    const int steps = (p.ka + K - 1) / K + (p.kb + K - 1) / K;
+    if (lin_place(blockIdx.x, p.tiles_m).row * BM >= p.n) return;
+    auto key_x = [](int r) { return r & 7; };
+    auto key_w = [](int r) { return weight_key<T>(r); };
 
-    // a lane's rows, from the block's first one on, and its places in them, in bytes
-    const int rows_here = p.n - row0 < BM ? (int)(p.n - row0) : BM, cols_here = p.m - col0 < BN ? p.m - col0 : BN;
-    int xr[LX], xc[LX], wc[LW];
-    uint32_t xo[LX], wo[LW];
-#pragma unroll
-    for (int i = 0; i < LX; ++i) {
-        const int r = (i * waves + wave) * RW + lane / C;
-        xr[i] = r < rows_here ? r : rows_here - 1;
-        xc[i] = ((lane % C) ^ key_x(r)) * V;
-        xo[i] = (uint32_t)((uint32_t)xr[i] * (uint32_t)p.lda + (uint32_t)xc[i]) * (uint32_t)sizeof(T);
-    }
-#pragma unroll
-    for (int i = 0; i < LW; ++i) {
-        const int r = (i * waves + wave) * RW + lane / C;
-        wc[i] = ((lane % C) ^ key_w(r)) * V;
-        wo[i] = (uint32_t)((uint32_t)(r < cols_here ? r : cols_here - 1) * (uint32_t)p.ldw + (uint32_t)wc[i]) * (uint32_t)sizeof(T);
-    }
-    const char *x = (const char*)((const T*)p.a + row0 * p.lda), *w = (const char*)((const T*)p.w + (int64_t)col0 * p.ldw);
-    int k = 0, d = p.ka, slot = 0;             // where the next step to load starts, in its source of width d
-    auto load = [&]() {
-        if (k >= d) {                          // on to b
-            x = (const char*)((const T*)p.b + row0 * p.ldb);
-            w = (const char*)((const T*)p.w + (int64_t)col0 * p.ldw + p.ka);
-            k = 0;
+    // The lane's place in what its load instructions bring: row r of the first one, `gap` rows from each to the next (a multiple of what the
+    // keys look at, so that a lane's columns are the same in all); the rows' places are computed anew for every load (a row and a stride in
+    // bytes are numbers of 24 bits), the registers are wanted for the sums.
+    constexpr int gap = RW * waves;
+    static_assert(gap % 32 == 0 && S == 2, "");
+    const int r0 = wave * RW + lane / C, xc = ((lane % C) ^ key_x(r0)) * V, wc = ((lane % C) ^ key_w(r0)) * V;
+    // What is loaded: the steps of this workgroup's tiles, one after the other, two steps ahead of the products; where the next one starts, in
+    // its source of width d, and zeros once the tiles have ended.
+    const char *x = nullptr, *w = nullptr;
+    int k = 0, d = 0, last_x = 0, last_w = 0;
+    uint32_t ldx = 0, coming = blockIdx.x;
+    const uint32_t ldw = (uint32_t)p.ldw * (uint32_t)sizeof(T);
+    bool second = false;                       // of [a | b]
+    auto next_source = [&]() {
+        k = 0;
+        if (d > 0 && !second && p.kb) {
+            second = true;
+            const LinPlace at = lin_place(coming - gridDim.x, p.tiles_m);
+            x = (const char*)((const T*)p.b + at.row * BM * p.ldb);
+            w = (const char*)((const T*)p.w + (int64_t)at.col * BN * p.ldw + p.ka);
+            ldx = (uint32_t)p.ldb * (uint32_t)sizeof(T);
             d = p.kb;
-#pragma unroll
-            for (int i = 0; i < LX; ++i) xo[i] = (uint32_t)((uint32_t)xr[i] * (uint32_t)p.ldb + (uint32_t)xc[i]) * (uint32_t)sizeof(T);
+            return;
         }
-        u32x4* to = stage[slot] + wave * 64;
-        const char *xk = x + (size_t)k * sizeof(T), *wk = w + (size_t)k * sizeof(T);
-        if (k + K <= d) {
-#pragma unroll
-            for (int i = 0; i < LX; ++i) __builtin_amdgcn_global_load_lds((mem_void*)(xk + xo[i]), (lds_void*)(to + i * waves * 64), 16, 0, 0);
-#pragma unroll
-            for (int i = 0; i < LW; ++i)
-                __builtin_amdgcn_global_load_lds((mem_void*)(wk + wo[i]), (lds_void*)(to + BM * C + i * waves * 64), 16, 0, 0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LX; ++i) {
-                const void* from = k + xc[i] < d ? (const void*)(xk + xo[i]) : (const void*)lin_zeros;
-                __builtin_amdgcn_global_load_lds((mem_void*)from, (lds_void*)(to + i * waves * 64), 16, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < LW; ++i) {
-                const void* from = k + wc[i] < d ? (const void*)(wk + wo[i]) : (const void*)lin_zeros;
-                __builtin_amdgcn_global_load_lds((mem_void*)from, (lds_void*)(to + BM * C + i * waves * 64), 16, 0, 0);
-            }
-        }
-        k += K;
-        slot = slot + 1 == S ? 0 : slot + 1;
+        second = false;
+        d = 0;
+        const LinPlace at = lin_place(coming, p.tiles_m);
+        const int64_t row = at.row * BM;
+        const int col = at.col * BN;
+        if (coming >= total || row >= p.n) return;
+        coming += gridDim.x;
+        last_x = p.n - row < BM ? (int)(p.n - row) - 1 : BM - 1;
+        last_w = p.m - col < BN ? p.m - col - 1 : BN - 1;
+        x = (const char*)((const T*)p.a + row * p.lda);
+        w = (const char*)((const T*)p.w + (int64_t)col * p.ldw);
+        ldx = (uint32_t)p.lda * (uint32_t)sizeof(T);
+        d = p.ka;
+    };
+    // load instruction i of a step, into buffer `to`
+    auto load = [&](u32x4* to, int i) {
+        const bool rows = i < LX;
+        const int q = rows ? i : i - LX, at = r0 + q * gap, last = rows ? last_x : last_w, c = rows ? xc : wc;
+        const void* from = (rows ? x : w) + (size_t)k * sizeof(T) +
+                           (__umul24((uint32_t)(at < last ? at : last), rows ? ldx : ldw) + (uint32_t)c * (uint32_t)sizeof(T));
+        from = k + c < d ? from : lin_zeros;
+        __builtin_amdgcn_global_load_lds((mem_void*)from, (lds_void*)(to + wave * 64 + (rows ? 0 : BM * C) + q * waves * 64), 16, 0, 0);
     };
 
+    // Operands: the rows' are read again for the next half step as soon as the last product with them is under way, the weights' have two
+    // sets of registers.
+    constexpr int J = V / 4;
+    const int wr = weight_row<T>(0, rho), px0 = (wm + rho) * C, pw0 = BM * C + (wn + wr) * C;
+    const int px[2] = {px0 + (g ^ key_x(rho)), px0 + ((4 + g) ^ key_x(rho))}, pw[2] = {pw0 + (g ^ key_w(wr)), pw0 + ((4 + g) ^ key_w(wr))};
+    u32x4 fx[MT], fw[2][NT];
     f32x4 acc[MT][NT];
+    auto read_x = [&](const u32x4* from, int h, int i) { fx[i] = from[px[h] + i * 16 * C]; };
+    auto read_w = [&](const u32x4* from, int h) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int j = 0; j < NT; ++j) fw[h][j] = from[pw[h] + (j / J * (4 * V) + j % J * 4) * C];
+    };
+    // Half h of a step, with the next half's rows from `next` and, where LOADS, a step's loads into `to`, dealt out between the products: sent
+    // at once they hold up the wave until the memory pipeline has taken them all.
+    auto multiply = [&](int h, const u32x4* next, u32x4* to, auto loads) {
+        constexpr bool LOADS = decltype(loads)::value;
+        constexpr int each = (LX + LW + MT - 1) / MT;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < S - 1 && s < steps; ++s) load();
-    int now = 0;
-    for (int s = 0; s < steps; ++s) {
-        if (s + S - 2 < steps) wait_loads_but<(S - 2) * (LX + LW)>();
-        else wait_loads_but<0>();
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) mma<T>(acc[i][j], fw[h][j], fx[i]);
+            read_x(next, h ^ 1, i);
+            if constexpr (LOADS)
+#pragma unroll
+                for (int q = i * each; q < (i + 1) * each; ++q)
+                    if (q < LX + LW) load(to, q);
+            __builtin_amdgcn_sched_barrier(0);     // as written
+        }
+    };
+
+    auto wait = [&](auto wait_loads) {
+        wait_loads();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + S - 1 < steps) load();
-        const u32x4 *sx = stage[now], *sw = sx + BM * C;
-        now = now + 1 == S ? 0 : now + 1;
+    };
+    // Loads and stores end in order.  A tile's second step was loaded before the tile before it was stored: the wait for it leaves the stores
+    // under way.  stored: how many store instructions there were at least (whole tiles; 0 where that is not known).
+    constexpr int stores = MT * NT * 4 / V;
+    int stored = 0, now = 0;
+    for (int q = 0; q < 2; ++q) {
+        if (k >= d) next_source();
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-            u32x4 fx[MT], fw[NT];
-            const int c = h * 4 + g;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int r = wm + i * 16 + rho;
-                fx[i] = sx[r * C + (c ^ key_x(r))];
-            }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int r = wn + weight_row<T>(j, rho);
-                fw[j] = sw[r * C + (c ^ key_w(r))];
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) mma<T>(acc[i][j], fw[j], fx[i]);
-        }
+        for (int i = 0; i < LX + LW; ++i) load(stage[q], i);
+        k += K;
     }
-    lin_epilogue<T, MT, NT, SPLIT>(acc, p, e, row0 + wm + rho, col0 + wn + g * V,
-                                       row0 + BM <= p.n && col0 + BN <= p.m);
+    wait([] { wait_loads_but<LX + LW>(); });
+    for (uint32_t id = blockIdx.x; id < total; id += gridDim.x) {
+        const LinPlace at = lin_place(id, p.tiles_m);
+        const int64_t row0 = at.row * BM;
+        const int col0 = at.col * BN;
+        if (row0 >= p.n) break;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        read_w(stage[now], 0);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) read_x(stage[now], 0, i);
+        for (int s = 0; s < steps; ++s) {
+            u32x4* here = stage[now];
+            now ^= 1;
+            const u32x4* next = stage[now];
+            read_w(here, 1);
+            multiply(0, here, nullptr, std::false_type{});
+            // everyone has read this step's second half, and the next step has come
+            wait([&] {
+                if (s > 0) wait_loads_but<0>();
+                else if (stored >= 2 * stores && 2 * stores < 64) wait_loads_but<2 * stores < 64 ? 2 * stores : 0>();
+                else if (stored >= stores) wait_loads_but<stores>();
+                else wait_loads_but<0>();
+            });
+            if (k >= d) next_source();
+            read_w(next, 0);
+            multiply(1, next, here, std::true_type{});
+            k += K;
+            asm volatile("" ::: "memory");             // (the reads stay on this side of the next wait)
+        }
+        const bool whole = row0 + BM <= p.n && col0 + BN <= p.m;
+        lin_epilogue<T, MT, NT, SPLIT>(acc, p, e, row0 + wm + rho, col0 + wn + g * V, whole);
+        if (SPLIT) stored = whole && e.out && e.out2 ? stores : 0;
+        else stored = !whole ? 0 : e.pre ? 2 * stores : stores;
+    }
+    wait_loads_but<0>();                                // (zeros that are on their way: LDS is another workgroup's after the end)
 }
 
 // ---- dw = dz^T [a | b] ----------------------------------------------------------------------------------------------------
@@ -772,17 +816,17 @@ template <class T, bool SPLIT> void lin_product(const Product& p, const Epilogue
         Product q = p;
         q.tiles_m = (int)((p.m + Tile::BN - 1) / Tile::BN);
         const int64_t blocks = (p.n + Tile::BM - 1) / Tile::BM;
-        const dim3 grid((unsigned)((blocks + 7) / 8 * 8 * q.tiles_m));
-        if (direct) hipLaunchKernelGGL((k_lin_direct<T, Tile, SPLIT>), grid, dim3(Tile::threads), 0, stream, q, e);
-        else hipLaunchKernelGGL((k_lin_product<T, Tile, SPLIT>), grid, dim3(Tile::threads), 0, stream, q, e);
+        const uint32_t total = (uint32_t)((blocks + 7) / 8 * 8 * q.tiles_m), once = 256u * Tile::per_cu;
+        if (direct) hipLaunchKernelGGL((k_lin_direct<T, Tile, SPLIT>), dim3(total < once ? total : once), dim3(Tile::threads), 0, stream, q, e, total);
+        else hipLaunchKernelGGL((k_lin_product<T, Tile, SPLIT>), dim3(total), dim3(Tile::threads), 0, stream, q, e);
     };
     // the largest tile of which there are enough for the CUs
     auto tiles = [&](int64_t t) { return ((p.n + t - 1) / t) * ((p.m + t - 1) / t); };
     // (floats: four times the instructions a step, so that the smaller tile's loads are hidden too)
     if constexpr (sizeof(T) == 2)
-        if (p.m > 128 && tiles(256) >= 192) return run(LinTile<256, 256, 128, 64, 2, 2>{});
-    if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64, 2, 2>{});
-    else run(LinTile<64, 64, 32, 32, 2, 2>{});
+        if (p.m > 128 && tiles(256) >= 192) return run(LinTile<256, 256, 128, 64>{});
+    if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64>{});
+    else run(LinTile<64, 64, 32, 32>{});
 }
 
 // the backward pass's workspace
