@@ -419,7 +419,7 @@ typedef struct grem_rows {
 /* Mean of the neighbours' rows inside partitions: out[v] = sum of x[u] / |N(v)|, u in N(v) = the entries of
  * row v whose label is v's own and not negative (labels: n int32, as a partition call leaves them; NULL = all
  * entries count).  Entries are counted as stored.  out[v] = 0 where N(v) is empty; rows of x that no counted entry names
- * are not read, whatever they hold.  counts_out: n int32, |N(v)|, or NULL.  nnz = rowptr[n], the length of colidx;
+ * are not read, whatever they hold; rows of x (of dout in the backward pass) are less than 2^32 values apart.  counts_out: n int32, |N(v)|, or NULL.  nnz = rowptr[n], the length of colidx;
  * labelled: whether labels are given. */
 size_t grem_neighbour_mean_bytes(int32_t type, int64_t n, int64_t nnz, int64_t d, int32_t labelled);
 int grem_neighbour_mean(const void *rowptr, int32_t rowptr_bits, const int32_t *colidx, int64_t nnz, int64_t n,

@@ -52,6 +52,12 @@ template <class T, int V, bool EVEN> __device__ __forceinline__ WordsOf<T, V> lo
     }
 }
 
+// a run that is known to be whole
+template <class T, int V> __device__ __forceinline__ WordsOf<T, V> whole_words(const T* __restrict__ at)
+{
+    return ((const typename Words<T, V>::Place*)at)->w;
+}
+
 template <class T, int V> __device__ __forceinline__ void to_floats(const WordsOf<T, V>& w, float (&f)[V])
 {
     T v[V];

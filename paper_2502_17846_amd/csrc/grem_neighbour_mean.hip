@@ -126,12 +126,15 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
     __shared__ int32_t list_of[kNmWaves][N];
     __shared__ float weight_of[WEIGHTED ? kNmWaves : 1][WEIGHTED ? N : 1];
     __shared__ int32_t off_of[kNmWaves][R + 1], vertex_of[kNmWaves][R];
+    __shared__ float scales_of[kNmWaves][R];
     __shared__ float open_of[G > 1 ? kNmWaves : 1][2][G][G > 1 ? L * V * C : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane / L, mine_c = (lane % L) * V;
     int32_t *list = list_of[wave], *off = off_of[wave], *vertices = vertex_of[wave];
+    float* scales = scales_of[wave];
     float* weights = weight_of[WEIGHTED ? wave : 0];
     auto& open = open_of[G > 1 ? wave : 0];
     const bool narrow = bytes && found[kNmWide] == 0u;
+    const uint32_t pitch = (uint32_t)ldx;
     // the vertices' order cut in eight, one for the workgroups of each chiplet (they go to the chiplets in turn)
     const int64_t share = order ? (n + 7) / 8 : n, base_at = order ? (int64_t)(blockIdx.x & 7u) * share : 0;
     const int64_t end_at = base_at + share < n ? base_at + share : n;
@@ -212,7 +215,12 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
         if (lane <= R) off[lane] = lane < rows ? before : kept;
         if (lane < R) vertices[lane] = v;
         nm_wave_sync();
-        if (counts_out && is_row && !cut && !walked) counts_out[v] = off[lane + 1] - off[lane];
+        if (is_row) {
+            const int32_t here = off[lane + 1] - off[lane];
+            scales[lane] = 1.0f / (float)(here > 1 ? here : 1);
+            if (counts_out && !cut && !walked) counts_out[v] = here;
+        }
+        nm_wave_sync();
 
         for (int c0 = 0; c0 < d; c0 += L * V * C) {
             const int c = c0 + mine_c;
@@ -225,7 +233,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                     store_floats<T, V, EVEN>(out + to * ldo, c + k * L * V, d, acc[k]);
                 }
             };
-            auto scale_of = [&](int r) { return WEIGHTED ? 1.0f : 1.0f / (float)(off[r + 1] - off[r]); };
+            auto scale_of = [&](int r) { return WEIGHTED ? 1.0f : scales[r]; };
             const int stretch = (kept + G - 1) / G;
             const int j0 = part * stretch < kept ? part * stretch : kept, j1 = j0 + stretch < kept ? j0 + stretch : kept;
             int r = 0;
@@ -241,11 +249,16 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                 float g[U];
 #pragma unroll
                 for (int q = 0; q < U; ++q) {
-                    const int at = j + q < j1 ? j + q : j1 - 1, width = j + q < j1 ? d : 0;
-                    const int32_t u = list[at];
+                    // (what is read for a place beyond j1 is added to sums that have been stored)
+                    const int at = j + q < j1 ? j + q : j1 - 1;
+                    const T* from = x + (uint64_t)(uint32_t)list[at] * pitch;
                     g[q] = WEIGHTED ? weights[at] : 1.0f;
 #pragma unroll
-                    for (int k = 0; k < C; ++k) f[q][k] = load_words<T, V, EVEN>(x + (int64_t)u * ldx, c + k * L * V, width);
+                    for (int k = 0; k < C; ++k) {
+                        const int at_c = c + k * L * V;
+                        if constexpr (EVEN) f[q][k] = whole_words<T, V>(from + (at_c < d ? at_c : 0));
+                        else f[q][k] = load_words<T, V, false>(from, at_c, d);
+                    }
                 }
 #pragma unroll
                 for (int q = 0; q < U; ++q) {
@@ -584,7 +597,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
 {
     const int size = layer_size(type);
     if (!size || n < 0 || n > kLayerMaxRows || nnz < 0 || d < 1 || d > kLayerMaxCols || (bits != 32 && bits != 64) || (n && !rowptr) ||
-        (nnz && !colidx) || !layer_rows_ok(x, ldx, n, d, size) || !layer_rows_ok(out, ldo, n, d, size) || (weighted && n && !counts))
+        (nnz && !colidx) || !layer_rows_ok(x, ldx, n, d, size) || ldx > (int64_t)UINT32_MAX || !layer_rows_ok(out, ldo, n, d, size) || (weighted && n && !counts))
         return GREM_ERR_ARG;
     if (n == 0) return GREM_OK;
     const NmSpace s = nm_space(n, nnz, d, size, labels != nullptr);

@@ -123,3 +123,12 @@ def test_the_binding_takes_no_host_memory():
                  lambda: B.grem_checkpoint_unpack(B.Checkpoint(x.char(), x[:, :1].byte(), torch.float32))):
         with pytest.raises(TypeError, match="on the GPU"):
             call()
+
+
+def test_rows_too_far_apart_for_the_mean(lib):
+    order = "rowptr bits colidx nnz n labels type d x ldx out ldo counts ws bytes stream"
+    args = dict(rowptr=P, bits=64, colidx=P, nnz=100, n=10, labels=P, type=F32, d=64, x=P, ldx=1 << 32, out=P, ldo=64, counts=P, ws=None, bytes=0,
+                stream=None)
+    assert _call(lib.grem_neighbour_mean, order, args) == B.ERR_ARG
+    order = "rowptr bits colidx nnz n labels counts type d x ldx out ldo ws bytes stream"
+    assert _call(lib.grem_neighbour_mean_backward, order, args) == B.ERR_ARG
