@@ -740,7 +740,7 @@ def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     px, ldx = _matrix(x, dtype, n, d, "x")
     out, po, ldo = _into(stream, out, x, n, d, "out")
     mean, rstd = _new(stream, x, n, torch.float32), _new(stream, x, n, torch.float32)
-    rc = load().grem_layer_norm(t, n, d, px, ldx, _vector(gamma, dtype, d, "gamma"), _vector(beta, dtype, d, "beta"), eps, po, ldo,
+    rc = load().grem_layer_norm(t, n, d, px, ldx, _vector(gamma, dtype, d, "gamma"), _vector(beta, dtype, d, "beta"), float(eps), po, ldo,
                                 mean.data_ptr(), rstd.data_ptr(), _handle(stream, x))
     _check(rc, "grem_layer_norm")
     return out, mean, rstd

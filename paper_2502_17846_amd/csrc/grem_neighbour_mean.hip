@@ -22,7 +22,9 @@ constexpr int kNmBlock = 256;
 constexpr int kNmWaves = kNmBlock / 64;
 constexpr int kNmRows = 8;                      // vertices a wave takes at a time
 constexpr int kNmListed = 128;                  // entries of a row that goes on the list: the list holds kNmRows such rows
-constexpr int64_t kNmSegment = 128;             // entries that a long row is cut into, at least
+// entries that a long row is cut into, at least: as many as leave the few long rows of a small graph enough waves (500,000 entries x 128: 39 us,
+// with 192 44), from 2^20 entries on more of them, for fewer partial sums (2M entries x 64: 73 us with 128, 60 with 192)
+constexpr int64_t kNmSegmentFew = 128, kNmSegmentMany = 192, kNmManyEntries = 1 << 20;
 
 struct NmItem {
     int32_t row, segment;
@@ -475,8 +477,8 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const void* __restrict
     }
 }
 
-// A long row's segments added up, a workgroup a row: up to 32 segments a thread a column, more of them S threads a column over every S-th
-// segment, then those S in order.
+// A long row's segments added up, a row's columns dealt out over gridDim.y workgroups: up to 32 segments a thread a column, more of them S
+// threads a column over every S-th segment, then those S in order.  (One workgroup a row: 25 us at 7.9M entries x 256, the longest row's.)
 template <class T, bool WEIGHTED>
 __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __restrict__ found, const NmLong* __restrict__ longs,
                                                       const float* __restrict__ partial, const int32_t* __restrict__ part_counts,
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
             for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
             if (threadIdx.x == 0) {
                 total_of = total;
-                if (counts_out) counts_out[r.row] = total;
+                if (counts_out && blockIdx.y == 0) counts_out[r.row] = total;
             }
         }
         __syncthreads();
@@ -504,7 +506,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
         const float scale = WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1);
         const float* rowp = partial + (size_t)r.first * (size_t)d;
         if (r.count <= 32) {
-            for (int c = threadIdx.x; c < d; c += kNmBlock) {
+            for (int c = blockIdx.y * kNmBlock + threadIdx.x; c < d; c += gridDim.y * kNmBlock) {
                 float a = 0.0f;
 #pragma unroll 8
                 for (int s = 0; s < r.count; ++s) a += rowp[(size_t)s * (size_t)d + c];
@@ -513,7 +515,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
             __syncthreads();
             continue;
         }
-        for (int c0 = 0; c0 < d; c0 += W) {
+        for (int c0 = blockIdx.y * W; c0 < d; c0 += gridDim.y * W) {
             float a = 0.0f;
             if (c0 + i < d)
 #pragma unroll 8
@@ -549,7 +551,8 @@ NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
     int64_t most = ((int64_t)1 << 26) / d;
     most = most < 4096 ? 4096 : most > 65536 ? 65536 : most;
     s.segment = (nnz + most - 1) / most;
-    if (s.segment < kNmSegment) s.segment = kNmSegment;
+    const int64_t least = nnz < kNmManyEntries ? kNmSegmentFew : kNmSegmentMany;
+    if (s.segment < least) s.segment = least;
     // a row of e > segment entries has fewer than 2e / segment segments
     s.items = nnz > s.segment ? 2 * (nnz / s.segment) + 1 : 0;
     s.ordered = labelled && n * d * size >= kNmOrderedBytes;
@@ -567,7 +570,8 @@ NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
     return s;
 }
 
-// Vertices a wave takes: kNmRows where that still leaves every CU its 16 waves, fewer on smaller graphs.
+// Vertices a wave takes: kNmRows where that still leaves every CU its 16 waves, fewer on smaller graphs (10,000 x 100: rows 17.5 us with 2, 19.7
+// with 8).
 int nm_take(int64_t n)
 {
     int take = kNmRows;
@@ -612,7 +616,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
     const int64_t groups = (n + kNmWaves * take - 1) / (kNmWaves * take);
     const unsigned grid = (unsigned)(((groups < (1 << 22) ? groups : 1 << 22) + 7) / 8 * 8);
     const unsigned seg_grid = (unsigned)(s.items / kNmWaves + 1 < 2048 ? s.items / kNmWaves + 1 : 2048);
-    const unsigned join_grid = (unsigned)(s.items < 4096 ? s.items : 4096);
+    const unsigned join_grid = (unsigned)(s.items < 1024 ? s.items : 1024), join_cols = (unsigned)(d < 256 ? (d + 31) / 32 : 8);
     int32_t* order = nullptr;
     uint8_t* bytes = nullptr;
     if (s.ordered) {
@@ -636,7 +640,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
                 if (!s.items) return;
                 hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
                                    counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
-                hipLaunchKernelGGL((k_nm_join<T, W>), dim3(join_grid), dim3(kNmBlock), 0, stream, (int)d, found, longs, partial,
+                hipLaunchKernelGGL((k_nm_join<T, W>), dim3(join_grid, join_cols), dim3(kNmBlock), 0, stream, (int)d, found, longs, partial,
                                    part_counts, (T*)out, ldo, counts_out);
             };
             layer_either(d % kNmV<T> == 0, [&](auto even) { layer_either(weighted, [&](auto w) { run(even, w); }); });
