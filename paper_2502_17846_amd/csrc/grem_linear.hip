@@ -151,6 +151,29 @@ template <class T, bool WHOLE = false> __device__ __forceinline__ u32x4 chunk_of
     return r;
 }
 
+// A row's last run, where d is no multiple of V, is read as the V values that end at d, in one load, and moved down by the `over` values that
+// belong to the run before (a run beyond d: by V or more, nothing is left of it).  Loads stay under way until the runs are stored to LDS.
+template <class T> __device__ __forceinline__ int run_over(int k, int d)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    return k > d - V ? k - (d - V) : 0;
+}
+
+template <int BITS> __device__ __forceinline__ u32x4 moved_down(u32x4 v, int over)
+{
+    const int bits = over * BITS;
+    uint64_t w[2];
+    __builtin_memcpy(w, &v, 16);
+    const uint64_t from_high = bits < 64 ? w[1] << 1 << (63 - bits) : w[1] >> (bits & 63);
+    const uint64_t low = bits < 64 ? w[0] >> bits | from_high : bits < 128 ? from_high : 0ull;
+    const uint64_t high = bits < 64 ? w[1] >> bits : 0ull;
+    w[0] = low;
+    w[1] = high;
+    u32x4 r;
+    __builtin_memcpy(&r, w, 16);
+    return r;
+}
+
 // where row rho of the weights' operand j stands among a wave's features, and what tells the rows apart that are read together
 template <class T> __device__ __forceinline__ int weight_row(int j, int rho)
 {
@@ -275,6 +298,8 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
         wrow[i] = c < p.m ? c : p.m - 1;
     }
     u32x4 rx[LA], rw[LW];
+    int over = 0;
+    bool ragged = false;
     auto load = [&](int step) {
         const bool first = step < steps_a;
         const T* x = (const T*)(first ? p.a : p.b);
@@ -288,10 +313,28 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
 #pragma unroll
             for (int i = 0; i < LW; ++i) rw[i] = chunk_of<T, W>(w + wrow[i] * p.ldw, k, d);
         };
-        if (k - sc * V + K <= d) all(std::true_type{});
-        else all(std::false_type{});
+        over = 0;
+        ragged = false;
+        if (k - sc * V + K <= d) {
+            all(std::true_type{});
+        } else if (d >= V) {
+            over = run_over<T>(k, d);
+            ragged = true;
+#pragma unroll
+            for (int i = 0; i < LA; ++i) rx[i] = chunk_of<T, true>(x + xrow[i] * ld, k - over, d);
+#pragma unroll
+            for (int i = 0; i < LW; ++i) rw[i] = chunk_of<T, true>(w + wrow[i] * p.ldw, k - over, d);
+        } else {
+            all(std::false_type{});
+        }
     };
     auto store = [&](int buf) {
+        if (ragged) {
+#pragma unroll
+            for (int i = 0; i < LA; ++i) rx[i] = moved_down<8 * (int)sizeof(T)>(rx[i], over);
+#pragma unroll
+            for (int i = 0; i < LW; ++i) rw[i] = moved_down<8 * (int)sizeof(T)>(rw[i], over);
+        }
 #pragma unroll
         for (int i = 0; i < LA; ++i) sx[buf][(i * RS + sr) * 8 + (sc ^ (sr & 7))] = rx[i];
 #pragma unroll
@@ -530,6 +573,9 @@ template <class T, bool CK> struct Staged {
     {
         v = WHOLE || c < d ? chunk_of<T, WHOLE>((const T*)x.data + r * x.stride, c, d) : u32x4{0, 0, 0, 0};
     }
+    // the run at column c, read from `over` columns before it
+    __device__ __forceinline__ void load_over(const Rows& x, int64_t r, int c, int, int over) { v = chunk_of<T, true>((const T*)x.data + r * x.stride, c - over, 0); }
+    __device__ __forceinline__ void move_down(int over) { v = moved_down<8 * (int)sizeof(T)>(v, over); }
     __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
     __device__ __forceinline__ u32x4 values() const { return v; }
 };
@@ -557,6 +603,18 @@ template <class T> struct Staged<T, true> {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = c + i < d ? row[c + i] : (int8_t)0;
         __builtin_memcpy(&q, v, V);
+    }
+    __device__ __forceinline__ void load_over(const Rows& x, int64_t r, int c, int d, int over)
+    {
+        byte = x.exponents[r * x.exponent_stride + (c < d ? c : d - 1) / kCkGroup];
+        q = ((const Run8*)((const int8_t*)x.data + r * x.stride + (c - over)))->q;
+    }
+    __device__ __forceinline__ void move_down(int over)
+    {
+        uint64_t w = 0;
+        __builtin_memcpy(&w, &q, V);
+        w = over < V ? w >> (8 * over) : 0ull;
+        __builtin_memcpy(&q, &w, V);
     }
     __device__ __forceinline__ void clear()
     {
@@ -598,7 +656,11 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_weight(const T* __restric
 
     u32x4 rz[LM];
     Staged<T, CK> rx[LN];
-    const bool cols_whole = col0 + BM <= m && k0 + BN <= kd;
+    const bool cols_whole = col0 + BM <= m && k0 + BN <= kd, wide = m >= V && kd >= V;
+    static_assert(threads % CM == 0 && threads % CN == 0, "");          // a thread's runs all start at one column
+    const int cz = col0 + ((int)threadIdx.x % CM) * V, cx = k0 + ((int)threadIdx.x % CN) * V;
+    const int oz = wide ? run_over<T>(cz, m) : 0, ox = wide ? run_over<T>(cx, kd) : 0;
+    bool ragged = false;
     auto load = [&](int64_t from) {
         auto all = [&](auto whole) {
             constexpr bool W = decltype(whole)::value;
@@ -614,10 +676,26 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_weight(const T* __restric
                 else rx[i].clear();
             }
         };
-        if (cols_whole && from + R <= hi) all(std::true_type{});
-        else all(std::false_type{});
+        ragged = false;
+        if (cols_whole && from + R <= hi) {
+            all(std::true_type{});
+        } else if (wide && from + R <= hi) {
+            ragged = true;
+#pragma unroll
+            for (int i = 0; i < LM; ++i) rz[i] = chunk_of<T, true>(dz + (from + (i * threads + (int)threadIdx.x) / CM) * lddz, cz - oz, m);
+#pragma unroll
+            for (int i = 0; i < LN; ++i) rx[i].load_over(x, from + (i * threads + (int)threadIdx.x) / CN, cx, kd, ox);
+        } else {
+            all(std::false_type{});
+        }
     };
     auto store = [&](int buf) {
+        if (ragged) {
+#pragma unroll
+            for (int i = 0; i < LM; ++i) rz[i] = moved_down<8 * (int)sizeof(T)>(rz[i], oz);
+#pragma unroll
+            for (int i = 0; i < LN; ++i) rx[i].move_down(ox);
+        }
 #pragma unroll
         for (int i = 0; i < LM; ++i) {
             const int q = i * threads + (int)threadIdx.x;
@@ -727,7 +805,7 @@ template <class T, bool EVEN, int ACT> __device__ __forceinline__ void lin_slope
                 to_floats<T, V>(wz, z);
 #pragma unroll
                 for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(z[i]);
-                store_floats<T, V, EVEN>(p.dz + r * p.lddz, c, m, f);
+                store_floats<T, V, true>(p.dz + r * p.lddz, c, m, f);          // (zeros up to lddz)
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) s[i] += f[i];
@@ -745,7 +823,8 @@ template <class T, bool EVEN, int ACT> __device__ __forceinline__ void lin_slope
     }
 }
 
-// w (m x width) turned: wt (width x m), so that dz w is a product of the first kind
+// w (m x width) turned: wt (width x m, zeros up to ldt), so that dz w is a product of the first kind; dz and wt are both filled up with zeros to
+// whole runs, and the product takes those as well
 template <class T> struct Turn {
     const T* w;
     T* wt;
@@ -764,7 +843,7 @@ template <class T> __device__ __forceinline__ void lin_turn(const Turn<T>& p, ui
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 32; i += 8)
-        if (c0 + y + i < p.width && f0 + x < p.m) p.wt[(int64_t)(c0 + y + i) * p.ldt + f0 + x] = tile[x][y + i];
+        if (c0 + y + i < p.width && f0 + x < p.ldt) p.wt[(int64_t)(c0 + y + i) * p.ldt + f0 + x] = f0 + x < p.m ? tile[x][y + i] : (T)0.0f;
 }
 
 // What the products wait for, in one launch: the turned weights' workgroups first, dz's after them.
@@ -954,7 +1033,8 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
             }
         }
         if (turned) {
-            const Product p{dz, nullptr, wt, lddz, 0, s.ldt, n, (int)m, 0, (int)(ka + kb), 0};
+            const int inner = activation != GREM_ACT_NONE ? (int)s.lddz : (int)m;
+            const Product p{dz, nullptr, wt, lddz, 0, s.ldt, n, inner, 0, (int)(ka + kb), 0};
             const Epilogue e{nullptr, nullptr, da, nullptr, db, 0, ldda, 0, lddb, (int)ka, GREM_ACT_NONE};
             lin_product<T, true>(p, e, stream);
         }
