@@ -7,13 +7,17 @@
 // hold a row in at most 4 runs of 16 bytes a lane) takes a row, keeps it in registers, and the variance is summed about the mean: x is read
 // once and no digits cancel.  The backward pass walks rows with the columns' two sums in registers, too; a workgroup leaves one partial row of
 // each, and k_ln_join adds those in a fixed order (no atomics: the same bytes on every run).
+// 1M x 256 bfloat16: 218 us, 4.9 TB/s; the backward pass of 262,144 x 1,024 from 8 bits 262 us, 5.2 TB/s (a copy: 4.9-5.4).
 #include "grem_layers.hip.h"
 
 namespace {
 
 constexpr int kLnBlock = 256;
-constexpr int kLnGroups = 768;                  // workgroups of the backward pass, at most: each leaves 8d bytes (three a CU: 1,024 of them
-                                                // end in a second round that is mostly empty, 301 us for 280 at 262,144 x 1,024)
+// Workgroups of the backward pass, at most; each leaves 8d bytes.  Three a CU where a row fills a wave or more (1,024 of them end in a second
+// round that is mostly empty, 301 us for 280 at 262,144 x 1,024); narrow rows are few bytes a wave and need eight a CU under way
+// (500,000 x 100: 111 us for 124; 1M x 256 would lose by them, 326 us for 288).
+constexpr int64_t kLnNarrow = 128;
+constexpr int ln_groups(int64_t d) { return d <= kLnNarrow ? 2048 : 768; }
 
 template <class T> constexpr int kLnV = 16 / (int)sizeof(T);
 
@@ -375,7 +379,7 @@ extern "C" int grem_layer_norm(int32_t type, int64_t n, int64_t d, const void* x
 extern "C" size_t grem_layer_norm_backward_bytes(int64_t n, int64_t d)
 {
     if (n < 0 || n > kLayerMaxRows || d < 1 || d > kLayerMaxCols) return 0;
-    return layer_align((size_t)(n < kLnGroups ? n : kLnGroups) * 2 * (size_t)d * sizeof(float));
+    return layer_align((size_t)(n < ln_groups(d) ? n : ln_groups(d)) * 2 * (size_t)d * sizeof(float));
 }
 
 extern "C" int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, const void* dy, int64_t lddy, const grem_rows* x,
@@ -397,12 +401,12 @@ extern "C" int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, cons
         using T = decltype(t);
         auto run = [&](auto packed) {
             constexpr bool CK = decltype(packed)::value;
-            int parts = (int)(n < kLnGroups ? n : kLnGroups);
+            int parts = (int)(n < ln_groups(d) ? n : ln_groups(d));
             if (n) {
                 const bool held = ln_shaped<T>(d, [&](auto shape) {
                     constexpr int L = decltype(shape)::L, C = decltype(shape)::C;
                     const int64_t groups = (n * L + kLnBlock - 1) / kLnBlock;
-                    parts = (int)(groups < kLnGroups ? groups : kLnGroups);
+                    parts = (int)(groups < ln_groups(d) ? groups : ln_groups(d));
                     layer_either(d % kLnV<T> == 0, [&](auto even) {
                         hipLaunchKernelGGL((k_ln_backward<T, CK, decltype(even)::value, L, C>), dim3((unsigned)parts), dim3(kLnBlock), 0, stream,
                                            (const T*)dy, lddy, layer_rows(x), n, (int)d, mean, rstd, (const T*)gamma, (T*)dx, lddx, partial);

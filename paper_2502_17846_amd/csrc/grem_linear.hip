@@ -556,6 +556,8 @@ __global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(T
 
 // ---- dw = dz^T [a | b] ----------------------------------------------------------------------------------------------------
 //
+// 65,536 rows, 1,024 features by 2,048 columns from 8 bits: 300 us, 917 TFLOP/s; the operands' way through registers (where codes become values)
+// and the turning reads, not the products, bound it.
 // The long axis is the rows: a workgroup takes BM features of dz by BN columns of a or of b and a stretch of rows, and leaves its sums in
 // 32 bits; k_lin_join adds the stretches in order.  Both operands lie with the long axis across their rows.  They are staged as
 // they lie, and the reads from LDS turn them: for 16 bits the transposing read gives lane rho of 16 lanes four rows of column rho, where
