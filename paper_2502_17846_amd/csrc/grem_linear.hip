@@ -906,7 +906,8 @@ template <class T, bool SPLIT> void lin_product(const Product& p, const Epilogue
     // (floats: four times the instructions a step, so that the smaller tile's loads are hidden too)
     if constexpr (sizeof(T) == 2)
         if (p.m > 128 && tiles(256) >= 192) return run(LinTile<256, 256, 128, 64>{});
-    if (p.m > 64 && tiles(128) >= 192) run(LinTile<128, 128, 64, 64>{});
+    // (and beyond 2^29 rows of few features: a launch takes fewer than 2^32 threads)
+    if ((p.m > 64 || p.n > (1 << 29)) && tiles(128) >= 192) run(LinTile<128, 128, 64, 64>{});
     else run(LinTile<64, 64, 32, 32>{});
 }
 
