@@ -46,11 +46,15 @@ __device__ __forceinline__ int64_t nm_start(const void* __restrict__ rowptr, int
     return bits == 64 ? ((const int64_t*)rowptr)[v] : (int64_t)((const int32_t*)rowptr)[v];
 }
 
-__device__ __forceinline__ float nm_weight(const int32_t* __restrict__ counts, int32_t u)
-{
-    const int32_t k = counts[u];
-    return 1.0f / (float)(k > 1 ? k : 1);
-}
+__device__ __forceinline__ float nm_size(int32_t count) { return (float)(count > 1 ? count : 1); }
+
+// The sum of a row of the forward pass over its count, divided: a sum times the rounded 1/count is off by one rounding more, and falls beside
+// the ties between 16-bit values (41 ones have 0.99999994 for their mean).
+template <bool WEIGHTED> __device__ __forceinline__ float nm_mean(float sum, float size) { return WEIGHTED ? sum : sum / size; }
+
+// An entry's weight in the backward pass, rounded once; its product with a value is not rounded (it is added in the same instruction), so a term
+// is off by as much as the rounded quotient is.
+__device__ __forceinline__ float nm_weight(const int32_t* __restrict__ counts, int32_t u) { return 1.0f / nm_size(counts[u]); }
 
 // Adds up the counted entries of [lo, hi) for columns [c0, c0 + L*V*C); every lane ends with the sums of its columns over its own
 // neighbours.  Returns how many entries counted.
@@ -130,11 +134,11 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
     __shared__ int32_t list_of[kNmWaves][N];
     __shared__ float weight_of[WEIGHTED ? kNmWaves : 1][WEIGHTED ? N : 1];
     __shared__ int32_t off_of[kNmWaves][R + 1], vertex_of[kNmWaves][R];
-    __shared__ float scales_of[kNmWaves][R];
+    __shared__ float sizes_of[kNmWaves][R];
     __shared__ float open_of[G > 1 ? kNmWaves : 1][2][G][G > 1 ? L * V * C : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane / L, mine_c = (lane % L) * V;
     int32_t *list = list_of[wave], *off = off_of[wave], *vertices = vertex_of[wave];
-    float* scales = scales_of[wave];
+    float* sizes = sizes_of[wave];
     float* weights = weight_of[WEIGHTED ? wave : 0];
     auto& open = open_of[G > 1 ? wave : 0];
     const bool narrow = bytes && found[kNmWide] == 0u;
@@ -221,23 +225,22 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
         nm_wave_sync();
         if (is_row) {
             const int32_t here = off[lane + 1] - off[lane];
-            scales[lane] = 1.0f / (float)(here > 1 ? here : 1);
+            sizes[lane] = nm_size(here);
             if (counts_out && !cut && !walked) counts_out[v] = here;
         }
         nm_wave_sync();
 
         for (int c0 = 0; c0 < d; c0 += L * V * C) {
             const int c = c0 + mine_c;
-            auto store = [&](int32_t to, float (&acc)[C][V], float scale) {
+            auto store = [&](int32_t to, float (&acc)[C][V], float size) {
 #pragma unroll
                 for (int k = 0; k < C; ++k) {
                     if (c + k * L * V >= d) continue;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) acc[k][i] *= scale;
+                    for (int i = 0; i < V; ++i) acc[k][i] = nm_mean<WEIGHTED>(acc[k][i], size);
                     store_floats<T, V, EVEN>(out + to * ldo, c + k * L * V, d, acc[k]);
                 }
             };
-            auto scale_of = [&](int r) { return WEIGHTED ? 1.0f : scales[r]; };
             const int stretch = (kept + G - 1) / G;
             const int j0 = part * stretch < kept ? part * stretch : kept, j1 = j0 + stretch < kept ? j0 + stretch : kept;
             int r = 0;
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                     if (j + q + 1 == end) {
                         // the row's last entry in this stretch
                         if (G == 1 || (off[r] >= j0 && off[r + 1] <= j1)) {
-                            store(vertices[r], acc, scale_of(r));
+                            store(vertices[r], acc, sizes[r]);
                         } else {
                             float* to = open[off[r] >= j0 ? 1 : 0][part];
 #pragma unroll
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                         for (int k = 0; k < C; ++k)
 #pragma unroll
                             for (int i = 0; i < V; ++i) acc[k][i] += open[0][h][k * L * V + mine_c + i];
-                    store(vertices[r], acc, scale_of(r));
+                    store(vertices[r], acc, sizes[r]);
                 }
                 nm_wave_sync();
             }
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
             for (int q = part; q < rows; q += G)
-                if (bare >> q & 1) store(vertices[q], acc, 0.0f);
+                if (bare >> q & 1) store(vertices[q], acc, 1.0f);
             // rows too long for the list, one after the other
             for (unsigned long long left = __ballot(walked); left; left &= left - 1) {
                 const int q = __ffsll((long long)left) - 1;
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_rows(const void* __restrict__ r
                     for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
                 const int total = nm_walk<T, EVEN, WEIGHTED, L, C>(colidx, first, last, labels, __shfl(label, q), counts, x, ldx, c0, d, acc);
                 if (c0 == 0 && lane == 0 && counts_out) counts_out[vertices[q]] = total;
-                if (part == 0) store(vertices[q], acc, WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1));
+                if (part == 0) store(vertices[q], acc, nm_size(total));
             }
         }
         nm_wave_sync();
@@ -505,14 +508,14 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
         }
         __syncthreads();
         const int total = total_of;
-        const float scale = WEIGHTED ? 1.0f : 1.0f / (float)(total > 1 ? total : 1);
+        const float size = nm_size(total);
         const float* rowp = partial + (size_t)r.first * (size_t)d;
         if (r.count <= 32) {
             for (int c = blockIdx.y * kNmBlock + threadIdx.x; c < d; c += gridDim.y * kNmBlock) {
                 float a = 0.0f;
 #pragma unroll 8
                 for (int s = 0; s < r.count; ++s) a += rowp[(size_t)s * (size_t)d + c];
-                out[(int64_t)r.row * ldo + c] = (T)(a * scale);
+                out[(int64_t)r.row * ldo + c] = (T)nm_mean<WEIGHTED>(a, size);
             }
             __syncthreads();
             continue;
@@ -528,7 +531,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_join(int d, const uint32_t* __r
                 float all = 0.0f;
 #pragma unroll
                 for (int s = 0; s < S; ++s) all += sums[s][i];
-                out[(int64_t)r.row * ldo + c0 + i] = (T)(all * scale);
+                out[(int64_t)r.row * ldo + c0 + i] = (T)nm_mean<WEIGHTED>(all, size);
             }
             __syncthreads();
         }
