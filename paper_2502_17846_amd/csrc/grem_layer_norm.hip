@@ -355,7 +355,8 @@ extern "C" int grem_layer_norm(int32_t type, int64_t n, int64_t d, const void* x
 {
     const int size = layer_size(type);
     if (!size || n < 0 || n > kLayerMaxRows || d < 1 || d > kLayerMaxCols || !(eps >= 0.0) || !layer_rows_ok(x, ldx, n, d, size) ||
-        !layer_rows_ok(y, ldy, n, d, size) || (uintptr_t)gamma % size || (uintptr_t)beta % size)
+        !layer_rows_ok(y, ldy, n, d, size) || (uintptr_t)gamma % size || (uintptr_t)beta % size ||
+        !layer_aligned(mean, 4) || !layer_aligned(rstd, 4))
         return GREM_ERR_ARG;
     if (n == 0) return GREM_OK;
     hipStream_t stream = (hipStream_t)stream_;
@@ -389,12 +390,12 @@ extern "C" int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, cons
     const int size = layer_size(type);
     if (!size || n < 0 || n > kLayerMaxRows || d < 1 || d > kLayerMaxCols || !layer_rows_ok(dy, lddy, n, d, size) ||
         !layer_source_ok(x, n, d, size) || (n && (!mean || !rstd)) || (dx && !layer_rows_ok(dx, lddx, n, d, size)) ||
-        (uintptr_t)gamma % size || (uintptr_t)dgamma % size || (uintptr_t)dbeta % size)
+        (uintptr_t)gamma % size || (uintptr_t)dgamma % size || (uintptr_t)dbeta % size || !layer_aligned(mean, 4) || !layer_aligned(rstd, 4))
         return GREM_ERR_ARG;
     const bool params = dgamma || dbeta;
     if (!dx && !params) return GREM_OK;
     if (n == 0 && !params) return GREM_OK;
-    if (params && n && (!workspace || workspace_bytes < grem_layer_norm_backward_bytes(n, d))) return GREM_ERR_NOMEM;
+    if (const int rc = layer_space(workspace, workspace_bytes, params ? grem_layer_norm_backward_bytes(n, d) : 0)) return rc;
     hipStream_t stream = (hipStream_t)stream_;
     float* partial = params ? (float*)workspace : nullptr;
     layer_typed(type, [&](auto t) {

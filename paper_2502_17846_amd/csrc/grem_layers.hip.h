@@ -178,6 +178,17 @@ inline bool layer_rows_ok(const void* p, int64_t stride, int64_t n, int64_t d, i
     return n == 0 || (p && (uintptr_t)p % (uintptr_t)size == 0 && stride >= d);
 }
 
+// (null is aligned)
+inline bool layer_aligned(const void* p, int to) { return (uintptr_t)p % (uintptr_t)to == 0; }
+
+// a workspace of at least `need` bytes; one that is not needed is not looked at
+inline int layer_space(const void* workspace, size_t bytes, size_t need)
+{
+    if (need == 0) return GREM_OK;
+    if (!workspace || bytes < need) return GREM_ERR_NOMEM;
+    return layer_aligned(workspace, 256) ? GREM_OK : GREM_ERR_ARG;
+}
+
 inline bool layer_ck_ok(const grem_rows* x, int64_t n, int64_t d)
 {
     return n == 0 || (x->data && x->stride >= d && x->exponent_stride >= (d + kCkGroup - 1) / kCkGroup);

@@ -1020,7 +1020,7 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
         return GREM_ERR_ARG;
     if (!da && !db && !dw && !dbias) return GREM_OK;
     const LinSpace s = lin_space(size, n, m, ka, kb, activation);
-    if (s.bytes && (!workspace || workspace_bytes < s.bytes)) return GREM_ERR_NOMEM;
+    if (const int rc = layer_space(workspace, workspace_bytes, s.bytes)) return rc;
     if (n == 0 && !dw && !dbias) return GREM_OK;
     hipStream_t stream = (hipStream_t)stream_;
     uint8_t* ws = (uint8_t*)workspace;

@@ -606,11 +606,12 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
 {
     const int size = layer_size(type);
     if (!size || n < 0 || n > kLayerMaxRows || nnz < 0 || d < 1 || d > kLayerMaxCols || (bits != 32 && bits != 64) || (n && !rowptr) ||
-        (nnz && !colidx) || !layer_rows_ok(x, ldx, n, d, size) || ldx > (int64_t)UINT32_MAX || !layer_rows_ok(out, ldo, n, d, size) || (weighted && n && !counts))
+        (nnz && !colidx) || !layer_rows_ok(x, ldx, n, d, size) || ldx > (int64_t)UINT32_MAX || !layer_rows_ok(out, ldo, n, d, size) || (weighted && n && !counts) ||
+        !layer_aligned(rowptr, bits / 8) || !layer_aligned(colidx, 4) || !layer_aligned(labels, 4) || !layer_aligned(counts, 4) || !layer_aligned(counts_out, 4))
         return GREM_ERR_ARG;
     if (n == 0) return GREM_OK;
     const NmSpace s = nm_space(n, nnz, d, size, labels != nullptr);
-    if (s.bytes && (!workspace || workspace_bytes < s.bytes)) return GREM_ERR_NOMEM;
+    if (const int rc = layer_space(workspace, workspace_bytes, s.bytes)) return rc;
     uint8_t* ws = (uint8_t*)workspace;
     uint32_t* found = (uint32_t*)ws;
     NmItem* items = s.items ? (NmItem*)(ws + s.o_items) : nullptr;
