@@ -552,10 +552,18 @@ def grem_expected_cut_noalloc_max_n() -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _handle(stream, like: torch.Tensor):
+def _run(fn, here: int, stream, *args):
+    """The library's call, launched on GPU `here`, on `stream` or on that GPU's current one; raises where it fails."""
     if stream is not None:
-        return stream.cuda_stream
-    return _raw_stream(like.device.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
+        handle = stream.cuda_stream
+    else:
+        handle = _raw_stream(here) if _raw_stream else torch.cuda.current_stream(here).cuda_stream
+    if torch._C._cuda_getDevice() == here:
+        rc = fn(*args, handle)
+    else:
+        with torch.cuda.device(here):
+            rc = fn(*args, handle)
+    _check(rc, fn.__name__)
 
 
 def _new(stream, like: torch.Tensor, shape, dtype=None) -> torch.Tensor:
@@ -567,12 +575,12 @@ def _new(stream, like: torch.Tensor, shape, dtype=None) -> torch.Tensor:
     return like.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _into(stream, out: Optional[torch.Tensor], like: torch.Tensor, n: int, d: int, what: str):
+def _into(stream, out: Optional[torch.Tensor], like: torch.Tensor, here: int, n: int, d: int, what: str):
     """`out` checked, or a new matrix of `like`'s type; with its pointer and the values between its rows."""
     if out is None:
         out = _new(stream, like, (n, d))
         return out, out.data_ptr(), d
-    return (out, *_matrix(out, like.dtype, n, d, what))
+    return (out, *_matrix(out, here, like.dtype, n, d, what))
 
 
 def _space(stream, like: torch.Tensor, nbytes: int):
@@ -583,14 +591,30 @@ def _space(stream, like: torch.Tensor, nbytes: int):
     return buf, buf.data_ptr()
 
 
-def _first(t: torch.Tensor, what: str):
-    """(type, rows, columns) of the matrix whose type is the call's."""
+def _home(t: torch.Tensor, stream, what: str) -> int:
+    """The GPU of the call's first tensor: where the others and the stream have to be."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
+    here = t.get_device()
+    if stream is not None and stream.device_index != here:
+        raise ValueError(f"the stream is one of cuda:{stream.device_index}, {what} is on cuda:{here}")
+    return here
+
+
+def _at(t: torch.Tensor, here: int, what: str):
+    if not isinstance(t, torch.Tensor) or t.get_device() != here:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{what} must be a tensor on the GPU")
+        raise ValueError(f"{what} is on cuda:{t.get_device()}, the call's first tensor on cuda:{here}")
+
+
+def _first(t: torch.Tensor, stream, what: str):
+    """(GPU, type, rows, columns) of the matrix whose type is the call's."""
+    here = _home(t, stream, what)
     if t.dtype not in TYPES:
         raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
     n, d = _sides(t, what)
-    return TYPES[t.dtype], n, d
+    return here, TYPES[t.dtype], n, d
 
 
 def _sides(t: torch.Tensor, what: str):
@@ -600,10 +624,9 @@ def _sides(t: torch.Tensor, what: str):
     return shape
 
 
-def _matrix(t: torch.Tensor, dtype, n: int, d: int, what: str):
+def _matrix(t: torch.Tensor, here: int, dtype, n: int, d: int, what: str):
     """(pointer, values between rows) of a matrix whose rows' values lie side by side; rows may be any distance apart."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{what} must be a tensor on the GPU")
+    _at(t, here, what)
     if t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
     if t.shape != (n, d):
@@ -620,9 +643,10 @@ def _matrix(t: torch.Tensor, dtype, n: int, d: int, what: str):
     return t.data_ptr(), between
 
 
-def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str):
+def _vector(t: Optional[torch.Tensor], here: int, dtype, count: int, what: str):
     if t is None:
         return None
+    _at(t, here, what)
     if t.dim() != 1 or t.numel() != count:
         raise ValueError(f"{what} must have {count} entries, got shape {tuple(t.shape)}")
     return _dev(t, dtype, what)
@@ -632,20 +656,22 @@ def _width(t: Union[torch.Tensor, Checkpoint], what: str) -> int:
     return _sides(t.codes if isinstance(t, Checkpoint) else t, what)[1]
 
 
-def _source(t: Union[torch.Tensor, Checkpoint], dtype, n: int, d: int, what: str) -> Rows:
+def _source(t: Union[torch.Tensor, Checkpoint], here: int, dtype, n: int, d: int, what: str) -> Rows:
     """grem_rows of a matrix or of a checkpoint of that shape and type."""
     if not isinstance(t, Checkpoint):
-        p, ld = _matrix(t, dtype, n, d, what)
+        p, ld = _matrix(t, here, dtype, n, d, what)
         return Rows(p, ld, None, 0)
     if t.dtype != dtype:
         raise TypeError(f"{what} is a checkpoint of {t.dtype}, not of {dtype}")
-    p, ld = _matrix(t.codes, torch.int8, n, d, what + ".codes")
-    e, lde = _matrix(t.exponents, torch.uint8, n, -(-d // CHECKPOINT_GROUP), what + ".exponents")
+    p, ld = _matrix(t.codes, here, torch.int8, n, d, what + ".codes")
+    e, lde = _matrix(t.exponents, here, torch.uint8, n, -(-d // CHECKPOINT_GROUP), what + ".exponents")
     return Rows(p, ld, e, lde)
 
 
-def _graph(rowptr: torch.Tensor, colidx: torch.Tensor, n: int, what: str):
+def _graph(rowptr: torch.Tensor, colidx: torch.Tensor, here: int, n: int, what: str):
     """(rowptr's pointer, its bits, colidx's pointer, its length)"""
+    _at(rowptr, here, what)
+    _at(colidx, here, "colidx")
     if rowptr.numel() != n + 1:
         raise ValueError(f"{what} must have {n + 1} entries, got {rowptr.numel()}")
     return _dev(rowptr, rowptr.dtype, what), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel()
@@ -654,105 +680,98 @@ def _graph(rowptr: torch.Tensor, colidx: torch.Tensor, n: int, what: str):
 def grem_neighbour_mean(rowptr, colidx, n, x, labels=None, out=None, stream=None):
     """Returns (out (n, d), counts int32[n]): the mean over every vertex's neighbours of its own partition, and how many
     they are; without labels over all neighbours."""
-    t, _, d = _first(x, "x")
+    here, t, _, d = _first(x, stream, "x")
     lib = load()
-    px, ldx = _matrix(x, x.dtype, n, d, "x")
-    rp, bits, ci, nnz = _graph(rowptr, colidx, n, "rowptr")
-    out, po, ldo = _into(stream, out, x, n, d, "out")
+    px, ldx = _matrix(x, here, x.dtype, n, d, "x")
+    rp, bits, ci, nnz = _graph(rowptr, colidx, here, n, "rowptr")
+    out, po, ldo = _into(stream, out, x, here, n, d, "out")
     counts = _new(stream, x, n, torch.int32)
     nbytes = lib.grem_neighbour_mean_bytes(t, n, nnz, d, labels is not None)
     keep, ws = _space(stream, x, nbytes)
-    rc = lib.grem_neighbour_mean(rp, bits, ci, nnz, n, _vector(labels, torch.int32, n, "labels"), t, d, px, ldx, po, ldo,
-                                 counts.data_ptr(), ws, nbytes, _handle(stream, x))
-    _check(rc, "grem_neighbour_mean")
+    _run(lib.grem_neighbour_mean, here, stream, rp, bits, ci, nnz, n, _vector(labels, here, torch.int32, n, "labels"), t, d, px, ldx, po, ldo,
+         counts.data_ptr(), ws, nbytes)
     return out, counts
 
 
 def grem_neighbour_mean_backward(rowptr_t, colidx_t, n, dout, counts, labels=None, dx=None, stream=None) -> torch.Tensor:
     """dx (n, d) from dout and the forward call's counts; rowptr_t, colidx_t: the transposed graph (a symmetric one is its own)."""
-    t, _, d = _first(dout, "dout")
+    here, t, _, d = _first(dout, stream, "dout")
     lib = load()
-    pd, ldd = _matrix(dout, dout.dtype, n, d, "dout")
-    rp, bits, ci, nnz = _graph(rowptr_t, colidx_t, n, "rowptr_t")
-    dx, px, ldx = _into(stream, dx, dout, n, d, "dx")
+    pd, ldd = _matrix(dout, here, dout.dtype, n, d, "dout")
+    rp, bits, ci, nnz = _graph(rowptr_t, colidx_t, here, n, "rowptr_t")
+    dx, px, ldx = _into(stream, dx, dout, here, n, d, "dx")
     nbytes = lib.grem_neighbour_mean_bytes(t, n, nnz, d, labels is not None)
     keep, ws = _space(stream, dout, nbytes)
-    rc = lib.grem_neighbour_mean_backward(rp, bits, ci, nnz, n, _vector(labels, torch.int32, n, "labels"),
-                                          _vector(counts, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes,
-                                          _handle(stream, dout))
-    _check(rc, "grem_neighbour_mean_backward")
+    _run(lib.grem_neighbour_mean_backward, here, stream, rp, bits, ci, nnz, n, _vector(labels, here, torch.int32, n, "labels"),
+         _vector(counts, here, torch.int32, n, "counts"), t, d, pd, ldd, px, ldx, ws, nbytes)
     return dx
 
 
 def grem_linear(a, w, bias=None, b=None, act=ACT_NONE, residual=None, out=None, want_pre=False, stream=None):
     """act([a | b] w^T + bias) + residual, (n, m); with want_pre also z = [a | b] w^T + bias, as (out, z)."""
-    t, n, ka = _first(a, "a")
+    here, t, n, ka = _first(a, stream, "a")
     dtype, m, kb = a.dtype, _sides(w, "w")[0], 0
     pb, ldb, pr, ldr, z, pz, ldz = None, 0, None, 0, None, None, 0
-    pa, lda = _matrix(a, dtype, n, ka, "a")
+    pa, lda = _matrix(a, here, dtype, n, ka, "a")
     if b is not None:
         kb = _sides(b, "b")[1]
-        pb, ldb = _matrix(b, dtype, n, kb, "b")
-    pw, ldw = _matrix(w, dtype, m, ka + kb, "w")
+        pb, ldb = _matrix(b, here, dtype, n, kb, "b")
+    pw, ldw = _matrix(w, here, dtype, m, ka + kb, "w")
     if residual is not None:
-        pr, ldr = _matrix(residual, dtype, n, m, "residual")
-    out, po, ldo = _into(stream, out, a, n, m, "out")
+        pr, ldr = _matrix(residual, here, dtype, n, m, "residual")
+    out, po, ldo = _into(stream, out, a, here, n, m, "out")
     if want_pre:
-        z, pz, ldz = _into(stream, None, a, n, m, "pre")
-    rc = load().grem_linear(t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, dtype, m, "bias"), act, pr, ldr, po, ldo, pz, ldz,
-                            _handle(stream, a))
-    _check(rc, "grem_linear")
+        z, pz, ldz = _into(stream, None, a, here, n, m, "pre")
+    _run(load().grem_linear, here, stream, t, n, m, pa, lda, ka, pb, ldb, kb, pw, ldw, _vector(bias, here, dtype, m, "bias"), act, pr, ldr,
+         po, ldo, pz, ldz)
     return (out, z) if want_pre else out
 
 
 def grem_linear_backward(dout, a, w, b=None, act=ACT_NONE, pre=None, want_inputs=True, want_params=True, stream=None):
     """Returns (da, db, dw, dbias); db is None without b, and so are the inputs' or the parameters' gradients that are not
     wanted.  a, b: the forward call's inputs, or checkpoints of them; pre: its z (not used without an activation)."""
-    t, n, m = _first(dout, "dout")
+    here, t, n, m = _first(dout, stream, "dout")
     dtype, lib = dout.dtype, load()
     _sides(w, "w")
     ka, kb = _width(a, "a"), 0 if b is None else _width(b, "b")
-    pd, ldd = _matrix(dout, dtype, n, m, "dout")
-    pw, ldw = _matrix(w, dtype, m, ka + kb, "w")
-    ra, rb = _source(a, dtype, n, ka, "a"), None if b is None else _source(b, dtype, n, kb, "b")
+    pd, ldd = _matrix(dout, here, dtype, n, m, "dout")
+    pw, ldw = _matrix(w, here, dtype, m, ka + kb, "w")
+    ra, rb = _source(a, here, dtype, n, ka, "a"), None if b is None else _source(b, here, dtype, n, kb, "b")
     pz, ldz = None, 0
     if act != ACT_NONE:
         if pre is None:
             raise ValueError("an activation's backward pass needs pre")
-        pz, ldz = _matrix(pre, dtype, n, m, "pre")
-    da, pda, ldda = _into(stream, None, dout, n, ka, "da") if want_inputs else (None, None, 0)
-    db, pdb, lddb = _into(stream, None, dout, n, kb, "db") if want_inputs and kb else (None, None, 0)
-    dw, pdw, lddw = _into(stream, None, dout, m, ka + kb, "dw") if want_params else (None, None, 0)
+        pz, ldz = _matrix(pre, here, dtype, n, m, "pre")
+    da, pda, ldda = _into(stream, None, dout, here, n, ka, "da") if want_inputs else (None, None, 0)
+    db, pdb, lddb = _into(stream, None, dout, here, n, kb, "db") if want_inputs and kb else (None, None, 0)
+    dw, pdw, lddw = _into(stream, None, dout, here, m, ka + kb, "dw") if want_params else (None, None, 0)
     dbias = _new(stream, dout, m) if want_params else None
     nbytes = lib.grem_linear_backward_bytes(t, n, m, ka, kb, act)
     keep, ws = _space(stream, dout, nbytes)
-    rc = lib.grem_linear_backward(t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb), kb,
-                                  pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes,
-                                  _handle(stream, dout))
-    _check(rc, "grem_linear_backward")
+    _run(lib.grem_linear_backward, here, stream, t, n, m, pd, ldd, act, pz, ldz, ctypes.byref(ra), ka, None if rb is None else ctypes.byref(rb),
+         kb, pw, ldw, pda, ldda, pdb, lddb, pdw, lddw, None if dbias is None else dbias.data_ptr(), ws, nbytes)
     return da, db, dw, dbias
 
 
 def grem_layer_norm(x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
     """Returns (y (n, d), mean float32[n], rstd float32[n])."""
-    t, n, d = _first(x, "x")
+    here, t, n, d = _first(x, stream, "x")
     dtype = x.dtype
-    px, ldx = _matrix(x, dtype, n, d, "x")
-    out, po, ldo = _into(stream, out, x, n, d, "out")
+    px, ldx = _matrix(x, here, dtype, n, d, "x")
+    out, po, ldo = _into(stream, out, x, here, n, d, "out")
     mean, rstd = _new(stream, x, n, torch.float32), _new(stream, x, n, torch.float32)
-    rc = load().grem_layer_norm(t, n, d, px, ldx, _vector(gamma, dtype, d, "gamma"), _vector(beta, dtype, d, "beta"), float(eps), po, ldo,
-                                mean.data_ptr(), rstd.data_ptr(), _handle(stream, x))
-    _check(rc, "grem_layer_norm")
+    _run(load().grem_layer_norm, here, stream, t, n, d, px, ldx, _vector(gamma, here, dtype, d, "gamma"), _vector(beta, here, dtype, d, "beta"),
+         float(eps), po, ldo, mean.data_ptr(), rstd.data_ptr())
     return out, mean, rstd
 
 
 def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params=True, stream=None):
     """Returns (dx, dgamma, dbeta) (the last two None unless wanted); x: the forward call's input, or a checkpoint of it."""
-    t, n, d = _first(dy, "dy")
+    here, t, n, d = _first(dy, stream, "dy")
     dtype, lib = dy.dtype, load()
-    pd, ldd = _matrix(dy, dtype, n, d, "dy")
-    rx = _source(x, dtype, n, d, "x")
-    dx, px, ldx = _into(stream, dx, dy, n, d, "dx")
+    pd, ldd = _matrix(dy, here, dtype, n, d, "dy")
+    rx = _source(x, here, dtype, n, d, "x")
+    dx, px, ldx = _into(stream, dx, dy, here, n, d, "dx")
     dgamma = dbeta = pg = pb = keep = ws = None
     nbytes = 0
     if want_params:
@@ -760,36 +779,33 @@ def grem_layer_norm_backward(dy, x, mean, rstd, gamma=None, dx=None, want_params
         pg, pb = dgamma.data_ptr(), dbeta.data_ptr()
         nbytes = lib.grem_layer_norm_backward_bytes(n, d)
         keep, ws = _space(stream, dy, nbytes)
-    rc = lib.grem_layer_norm_backward(t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, torch.float32, n, "mean"),
-                                      _vector(rstd, torch.float32, n, "rstd"), _vector(gamma, dtype, d, "gamma"), px, ldx, pg, pb,
-                                      ws, nbytes, _handle(stream, dy))
-    _check(rc, "grem_layer_norm_backward")
+    _run(lib.grem_layer_norm_backward, here, stream, t, n, d, pd, ldd, ctypes.byref(rx), _vector(mean, here, torch.float32, n, "mean"),
+         _vector(rstd, here, torch.float32, n, "rstd"), _vector(gamma, here, dtype, d, "gamma"), px, ldx, pg, pb, ws, nbytes)
     return dx, dgamma, dbeta
 
 
 def grem_checkpoint_pack(x, stream=None) -> Checkpoint:
     """x's rows in 8 bits: groups of 32 columns, int8 codes and one exponent byte each."""
-    t, n, d = _first(x, "x")
-    px, ldx = _matrix(x, x.dtype, n, d, "x")
+    here, t, n, d = _first(x, stream, "x")
+    px, ldx = _matrix(x, here, x.dtype, n, d, "x")
     groups = -(-d // CHECKPOINT_GROUP)
     codes, exponents = _new(stream, x, (n, d), torch.int8), _new(stream, x, (n, groups), torch.uint8)
-    rc = load().grem_checkpoint_pack(t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups, _handle(stream, x))
-    _check(rc, "grem_checkpoint_pack")
+    _run(load().grem_checkpoint_pack, here, stream, t, n, d, px, ldx, codes.data_ptr(), d, exponents.data_ptr(), groups)
     return Checkpoint(codes, exponents, x.dtype)
 
 
 def grem_checkpoint_unpack(checkpoint: Checkpoint, out=None, stream=None) -> torch.Tensor:
     """The values that a checkpoint's codes stand for, in its type."""
     codes, exponents, dtype = checkpoint
+    here = _home(codes, stream, "checkpoint.codes")
     n, d = _sides(codes, "checkpoint.codes")
     if dtype not in TYPES:
         raise TypeError(f"a checkpoint is read back as float32, bfloat16 or float16, not {dtype}")
-    rx = _source(checkpoint, dtype, n, d, "checkpoint")
+    rx = _source(checkpoint, here, dtype, n, d, "checkpoint")
     if out is None:
         out = _new(stream, codes, (n, d), dtype)
         po, ldo = out.data_ptr(), d
     else:
-        po, ldo = _matrix(out, dtype, n, d, "out")
-    rc = load().grem_checkpoint_unpack(TYPES[dtype], n, d, ctypes.byref(rx), po, ldo, _handle(stream, codes))
-    _check(rc, "grem_checkpoint_unpack")
+        po, ldo = _matrix(out, here, dtype, n, d, "out")
+    _run(load().grem_checkpoint_unpack, here, stream, TYPES[dtype], n, d, ctypes.byref(rx), po, ldo)
     return out
