@@ -547,6 +547,9 @@ def grem_expected_cut_noalloc_max_n() -> int:
 
 
 # ---- layers on a partitioned graph ------------------------------------------------------------------------------
+#
+# Torch's automatic differentiation does not see these calls (each has a backward call of its own), so tensors that require gradients are
+# refused while it records.
 
 # the current stream's handle without a Stream object around it (2.7 us of a call's 14)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -606,6 +609,9 @@ def _at(t: torch.Tensor, here: int, what: str):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{what} must be a tensor on the GPU")
         raise ValueError(f"{what} is on cuda:{t.get_device()}, the call's first tensor on cuda:{here}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, and this call would not be recorded: detach it or call inside torch.no_grad(), and take "
+                         "the gradient from the operator's backward call")
 
 
 def _first(t: torch.Tensor, stream, what: str):
