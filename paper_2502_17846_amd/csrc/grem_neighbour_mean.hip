@@ -449,7 +449,8 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_order(const int32_t* __restrict
         if (lo + i * 64 < n) order[seen[wave][bin[i]] + rank[i]] = (int32_t)(lo + i * 64);
 }
 
-// the listed segments, a wave each: sums into partial (a row of d floats an item), counts beside them
+// the listed segments, a wave each: sums into partial (a row of d floats an item), counts beside them.  Of rows so wide that there are few segments
+// gridDim.y waves take a segment's columns in turn.
 template <class T, bool EVEN, bool WEIGHTED, int L, int C>
 __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const void* __restrict__ rowptr, int bits, const int32_t* __restrict__ colidx,
                                                           const int32_t* __restrict__ labels, const int32_t* __restrict__ counts,
@@ -464,7 +465,7 @@ __global__ __launch_bounds__(kNmBlock) void k_nm_segments(const void* __restrict
         const NmItem item = items[it];
         const int64_t lo = nm_start(rowptr, bits, item.row) + item.segment * segment, end = nm_start(rowptr, bits, (int64_t)item.row + 1);
         const int64_t hi = lo + segment < end ? lo + segment : end;
-        for (int c0 = 0; c0 < d; c0 += L * V * C) {
+        for (int c0 = (int)blockIdx.y * (L * V * C); c0 < d; c0 += (int)gridDim.y * (L * V * C)) {
             float acc[C][V];
 #pragma unroll
             for (int k = 0; k < C; ++k)
@@ -552,9 +553,9 @@ struct NmSpace {
 NmSpace nm_space(int64_t n, int64_t nnz, int64_t d, int size, bool labelled)
 {
     NmSpace s;
-    // as many segments as leave their sums in half a gigabyte, and no more than 65,536 or so: longer ones rather than more
+    // as many segments as leave their sums in half a gigabyte, and no more than 65,536 or so: longer ones rather than more (64 at a width of 2^20)
     int64_t most = ((int64_t)1 << 26) / d;
-    most = most < 4096 ? 4096 : most > 65536 ? 65536 : most;
+    if (most > 65536) most = 65536;
     s.segment = (nnz + most - 1) / most;
     const int64_t least = nnz < kNmManyEntries ? kNmSegmentFew : kNmSegmentMany;
     if (s.segment < least) s.segment = least;
@@ -621,6 +622,8 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
     const int take = nm_take(n);
     const int64_t groups = (n + kNmWaves * take - 1) / (kNmWaves * take);
     const unsigned grid = (unsigned)(((groups < (1 << 22) ? groups : 1 << 22) + 7) / 8 * 8);
+    // (a wave's columns are 512 at least)
+    const unsigned seg_cols = (unsigned)(d <= 16384 ? 1 : (d + 16383) / 16384);
     const unsigned seg_grid = (unsigned)(s.items / kNmWaves + 1 < 2048 ? s.items / kNmWaves + 1 : 2048);
     const unsigned join_grid = (unsigned)(s.items < 1024 ? s.items : 1024), join_cols = (unsigned)(d < 256 ? (d + 31) / 32 : 8);
     int32_t* order = nullptr;
@@ -644,7 +647,7 @@ int nm_run(const void* rowptr, int32_t bits, const int32_t* colidx, int64_t nnz,
                 hipLaunchKernelGGL((k_nm_rows<T, E, W, L, C>), dim3(grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, n, labels, counts,
                                    (const T*)x, ldx, (int)d, (T*)out, ldo, counts_out, s.segment, found, items, longs, order, bytes, take);
                 if (!s.items) return;
-                hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
+                hipLaunchKernelGGL((k_nm_segments<T, E, W, L, C>), dim3(seg_grid, seg_cols), dim3(kNmBlock), 0, stream, rowptr, bits, colidx, labels,
                                    counts, (const T*)x, ldx, (int)d, s.segment, found, items, partial, part_counts);
                 hipLaunchKernelGGL((k_nm_join<T, W>), dim3(join_grid, join_cols), dim3(kNmBlock), 0, stream, (int)d, found, longs, partial,
                                    part_counts, (T*)out, ldo, counts_out);
