@@ -470,7 +470,8 @@ int grem_layer_norm_backward(int32_t type, int64_t n, int64_t d, const void *dy,
  * [-130, 122] with |x| <= 127 * 2^e in the group; codes (int8) are x / 2^e to the nearest, ties to even, at most 63
  * where 64 * 2^e would leave the type's range; the byte is e + 130.  A group that holds a NaN or an infinity has byte 255
  * and codes 0, and is read back as NaN.  codes: n x d, ldc bytes apart; exponents: n x ceil(d / 32), lde apart.
- * Read back, a code is code * 2^e: off by at most 2^(e-1), a 127th to a 254th of the group's largest value. */
+ * Read back, a code is code * 2^e: off by at most 2^(e-1), a 127th to a 254th of the group's largest value; where that value is 63.5 * 2^e or more
+ * at the end of the type's range (e = 10 in half precision, 122 in the others) a code of 63 is off by less than 2^e. */
 int grem_checkpoint_pack(int32_t type, int64_t n, int64_t d, const void *x, int64_t ldx, int8_t *codes, int64_t ldc,
                          uint8_t *exponents, int64_t lde, void *stream);
 int grem_checkpoint_unpack(int32_t type, int64_t n, int64_t d, const grem_rows *x, void *y, int64_t ldy, void *stream);
