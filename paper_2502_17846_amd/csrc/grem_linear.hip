@@ -847,21 +847,28 @@ template <class T> struct Turn {
     const T* w;
     T* wt;
     int64_t ldw, ldt;
-    int m, width, across;           // tiles of 32 along the width
+    int m, width;
+    uint32_t across, tiles;         // tiles of 32 along the width, and in all
 };
 
-template <class T> __device__ __forceinline__ void lin_turn(const Turn<T>& p, uint32_t piece)
+// (a launch takes fewer than 2^32 threads: beyond this many tiles, 2^30 weights, a workgroup takes several)
+constexpr uint32_t kLinTurns = 1 << 20;
+
+template <class T> __device__ __forceinline__ void lin_turn(const Turn<T>& p, uint32_t first, uint32_t turns)
 {
     __shared__ T tile[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int c0 = (int)(piece % (uint32_t)p.across) * 32, f0 = (int)(piece / (uint32_t)p.across) * 32;
+    for (uint32_t piece = first; piece < p.tiles; piece += turns) {
+        const int c0 = (int)(piece % p.across) * 32, f0 = (int)(piece / p.across) * 32;
+        if (piece != first) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 32; i += 8)
-        if (f0 + y + i < p.m && c0 + x < p.width) tile[y + i][x] = p.w[(int64_t)(f0 + y + i) * p.ldw + c0 + x];
-    __syncthreads();
+        for (int i = 0; i < 32; i += 8)
+            if (f0 + y + i < p.m && c0 + x < p.width) tile[y + i][x] = p.w[(int64_t)(f0 + y + i) * p.ldw + c0 + x];
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 32; i += 8)
-        if (c0 + y + i < p.width && f0 + x < p.ldt) p.wt[(int64_t)(c0 + y + i) * p.ldt + f0 + x] = f0 + x < p.m ? tile[x][y + i] : (T)0.0f;
+        for (int i = 0; i < 32; i += 8)
+            if (c0 + y + i < p.width && f0 + x < p.ldt) p.wt[(int64_t)(c0 + y + i) * p.ldt + f0 + x] = f0 + x < p.m ? tile[x][y + i] : (T)0.0f;
+    }
 }
 
 // What the products wait for, in one launch: the turned weights' workgroups first, dz's after them.
@@ -869,7 +876,7 @@ template <class T, bool EVEN, int ACT>
 __global__ __launch_bounds__(kLinBlock) void k_lin_prepare(Slope<T> slope, Turn<T> turn, uint32_t turns)
 {
     if (blockIdx.x < turns) {
-        lin_turn<T>(turn, blockIdx.x);
+        lin_turn<T>(turn, blockIdx.x, turns);
     } else {
         const uint32_t at = blockIdx.x - turns;
         lin_slope<T, EVEN, ACT>(slope, (int)(at / (uint32_t)slope.across), (int)(at % (uint32_t)slope.across));
@@ -1035,10 +1042,11 @@ extern "C" int grem_linear_backward(int32_t type, int64_t n, int64_t m, const vo
         const bool slopes = n && (activation != GREM_ACT_NONE || dbias), turned = n && (da || db);
         if (slopes || turned) {
             T* made = (T*)(ws + s.o_dz);
-            const int across = (int)((m + kLinDzCols * V - 1) / (kLinDzCols * V)), tiles = (int)((ka + kb + 31) / 32);
+            const int across = (int)((m + kLinDzCols * V - 1) / (kLinDzCols * V));
+            const uint32_t wide = (uint32_t)((ka + kb + 31) / 32), tiles = wide * (uint32_t)((m + 31) / 32);
             const Slope<T> slope{(const T*)dout, (const T*)pre, made, ldd, ldp, s.lddz, n, bias_parts, (int)m, s.parts, across};
-            const Turn<T> turn{(const T*)w, wt, ldw, s.ldt, (int)m, (int)(ka + kb), tiles};
-            const uint32_t turns = turned ? (uint32_t)tiles * (uint32_t)((m + 31) / 32) : 0u;
+            const Turn<T> turn{(const T*)w, wt, ldw, s.ldt, (int)m, (int)(ka + kb), wide, tiles};
+            const uint32_t turns = !turned ? 0u : tiles < kLinTurns ? tiles : kLinTurns;
             const uint32_t grid = turns + (slopes ? (uint32_t)s.parts * (uint32_t)across : 0u);
             by_act(activation, [&](auto act) {
                 layer_either(m % V == 0, [&](auto even) {
