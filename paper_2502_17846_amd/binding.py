@@ -566,7 +566,8 @@ def _run(fn, here: int, stream, *args):
     else:
         with torch.cuda.device(here):
             rc = fn(*args, handle)
-    _check(rc, fn.__name__)
+    if rc != OK:
+        raise GremError(rc, fn.__name__)
 
 
 def _new(stream, like: torch.Tensor, shape, dtype=None) -> torch.Tensor:
@@ -605,9 +606,11 @@ def _home(t: torch.Tensor, stream, what: str) -> int:
 
 
 def _at(t: torch.Tensor, here: int, what: str):
-    if not isinstance(t, torch.Tensor) or t.get_device() != here:
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{what} must be a tensor on the GPU")
+    """Returns if t is on GPU `here` and no gradient of it is lost.  (Called only where one of the two is in doubt: a call has half a dozen
+    tensors, and a look at each is 0.1 us of its 11.)"""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a tensor on the GPU")
+    if t.get_device() != here:
         raise ValueError(f"{what} is on cuda:{t.get_device()}, the call's first tensor on cuda:{here}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient, and this call would not be recorded: detach it or call inside torch.no_grad(), and take "
@@ -632,7 +635,8 @@ def _sides(t: torch.Tensor, what: str):
 
 def _matrix(t: torch.Tensor, here: int, dtype, n: int, d: int, what: str):
     """(pointer, values between rows) of a matrix whose rows' values lie side by side; rows may be any distance apart."""
-    _at(t, here, what)
+    if not isinstance(t, torch.Tensor) or t.requires_grad or t.get_device() != here:
+        _at(t, here, what)
     if t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
     if t.shape != (n, d):
@@ -652,10 +656,13 @@ def _matrix(t: torch.Tensor, here: int, dtype, n: int, d: int, what: str):
 def _vector(t: Optional[torch.Tensor], here: int, dtype, count: int, what: str):
     if t is None:
         return None
-    _at(t, here, what)
-    if t.dim() != 1 or t.numel() != count:
+    if not isinstance(t, torch.Tensor) or t.requires_grad or t.get_device() != here:
+        _at(t, here, what)
+    if t.shape != (count,):
         raise ValueError(f"{what} must have {count} entries, got shape {tuple(t.shape)}")
-    return _dev(t, dtype, what)
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{what} must be contiguous {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
 def _width(t: Union[torch.Tensor, Checkpoint], what: str) -> int:
@@ -676,8 +683,9 @@ def _source(t: Union[torch.Tensor, Checkpoint], here: int, dtype, n: int, d: int
 
 def _graph(rowptr: torch.Tensor, colidx: torch.Tensor, here: int, n: int, what: str):
     """(rowptr's pointer, its bits, colidx's pointer, its length)"""
-    _at(rowptr, here, what)
-    _at(colidx, here, "colidx")
+    for t, name in ((rowptr, what), (colidx, "colidx")):
+        if not isinstance(t, torch.Tensor) or t.get_device() != here:
+            _at(t, here, name)
     if rowptr.numel() != n + 1:
         raise ValueError(f"{what} must have {n + 1} entries, got {rowptr.numel()}")
     return _dev(rowptr, rowptr.dtype, what), _rowptr_bits(rowptr), _colidx(colidx), colidx.numel()
