@@ -447,8 +447,9 @@ int grem_linear(int32_t type, int64_t n, int64_t m, const void *a, int64_t lda, 
 
 /* dz = dout * act'(z) (ReLU's slope at 0 is 0), [da | db] = dz w, dw = dz^T [a | b], dbias = the columns' sums of
  * dz; the residual's gradient is dout itself.  pre: z as grem_linear left it (unused without an activation).  a, b: the inputs, as they
- * were or both as checkpoints; read for dw only.  Any of da, db, dw, dbias may be NULL.  dz is rounded to the type
- * before the two products. */
+ * were or both as checkpoints; read for dw only.  Any of da, db, dw, dbias may be NULL.  With an activation dz is rounded to the type
+ * before the two products: in the 16-bit types da, db and dw are off by 1.41 times what their own rounding makes (of their norm 2.9e-4 for
+ * 2.1e-4 in half precision, 2.35e-3 for 1.66e-3 in bfloat16); dbias is summed before. */
 size_t grem_linear_backward_bytes(int32_t type, int64_t n, int64_t m, int64_t ka, int64_t kb, int32_t act);
 int grem_linear_backward(int32_t type, int64_t n, int64_t m, const void *dout, int64_t ldd, int32_t act,
                          const void *pre, int64_t ldp, const grem_rows *a, int64_t ka, const grem_rows *b, int64_t kb,

@@ -7,7 +7,8 @@
 // hold a row in at most 4 runs of 16 bytes a lane) takes a row, keeps it in registers, and the variance is summed about the mean: x is read
 // once and no digits cancel.  The backward pass walks rows with the columns' two sums in registers, too; a workgroup leaves one partial row of
 // each, and k_ln_join adds those in a fixed order (no atomics: the same bytes on every run).
-// 1M x 256 bfloat16: 218 us, 4.9 TB/s; the backward pass of 262,144 x 1,024 from 8 bits 262 us, 5.2 TB/s (a copy: 4.9-5.4).
+// 1M x 256 bfloat16: 221 to 244 us from one way of timing to another, 4.9 to 4.4 TB/s; the backward pass of 262,144 x 1,024 from 8 bits 262 to 268 us,
+// 5.2 to 5.0 TB/s (a copy: 4.9-5.4).
 #include "grem_layers.hip.h"
 
 namespace {
@@ -242,8 +243,8 @@ __global__ __launch_bounds__(kLnBlock) void k_ln_backward_wide(const T* __restri
             float g[V];
             load_floats<T, V>(dy + row * lddy, c, d, t);
             Held<T, CK, V> h;
-        h.template load<false>(x, row, c, d);
-        h.floats(xh);
+            h.template load<false>(x, row, c, d);
+            h.floats(xh);
             ln_param<T, V>(gamma, c, d, 1.0f, g);
 #pragma unroll
             for (int i = 0; i < V; ++i) {

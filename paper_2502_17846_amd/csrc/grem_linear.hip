@@ -5,8 +5,10 @@
 // a and b are read where they are: the columns of a are the first steps of the product's long axis, those of b the rest, so a vertex's
 // own row and its neighbours' mean need not be copied next to each other.
 //
-// Sums are held in 32 bits in the matrix cores' registers; z, out and the gradients are rounded once each.  dz is rounded to the
-// inputs' type before its two products, which take 16-bit operands (its error, half a step of that type, is of the size of the outputs' own).
+// Sums are held in 32 bits in the matrix cores' registers; z, out and the gradients are rounded once each.  With an activation dz is rounded to
+// the inputs' type before its two products, whose operands are 16 bits wide: a second error of the size of the outputs' own rounding, independent
+// of it, so that da, db and dw are off by 1.41 times as much (of their norm: half precision 2.9e-4 for 2.1e-4, bfloat16 2.35e-3 for 1.66e-3).
+// Two operands for dz, its rounding and what that left, would take it away and double the products.
 #include "grem_layers.hip.h"
 
 namespace {
@@ -400,8 +402,9 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
                                        row0 + BM <= p.n && col0 + BN <= p.m);
 }
 
-// The same product where every run of 16 bytes is whole and aligned: the steps go from memory straight to LDS, two steps ahead of the
-// products.  A wave's load instruction fills 8 rows of 128 bytes, in order of its lanes: chunk c of row r lies at c ^ key(r) because the lane
+// The same product where every run of 16 bytes is whole and aligned: the steps go from memory straight to LDS, into two buffers.  When a step's
+// first half has been multiplied its second half is in registers and its buffer free: the step after the next is sent for then, between the second
+// half's products, and waited for in the middle of the next step, half a step to one step later.  A wave's load instruction fills 8 rows of 128 bytes, in order of its lanes: chunk c of row r lies at c ^ key(r) because the lane
 // at that place asked for chunk c.  Beyond the end of the long axis a lane asks for zeros.
 //
 // What bounds it is that path: 65,536 x 2,048 by 1,024 takes 208 us without the loads and 223 without the products, and took 286 with a step's
@@ -443,8 +446,8 @@ __global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(T
     constexpr int gap = RW * waves;
     static_assert(gap % 32 == 0 && S == 2, "");
     const int r0 = wave * RW + lane / C, xc = ((lane % C) ^ key_x(r0)) * V, wc = ((lane % C) ^ key_w(r0)) * V;
-    // What is loaded: the steps of this workgroup's tiles, one after the other, two steps ahead of the products; where the next one starts, in
-    // its source of width d, and zeros once the tiles have ended.
+    // What is loaded: the steps of this workgroup's tiles, one after the other, a step and a half ahead of the products; where the next one
+    // starts, in its source of width d, and zeros once the tiles have ended.
     const char *x = nullptr, *w = nullptr;
     int k = 0, d = 0, last_x = 0, last_w = 0;
     uint32_t ldx = 0, coming = blockIdx.x;
@@ -572,8 +575,9 @@ __global__ __launch_bounds__(Tile::threads) __attribute__((amdgpu_waves_per_eu(T
 
 // ---- dw = dz^T [a | b] ----------------------------------------------------------------------------------------------------
 //
-// 65,536 rows, 1,024 features by 2,048 columns from 8 bits: 300 us, 917 TFLOP/s; the operands' way through registers (where codes become values)
-// and the turning reads, not the products, bound it.
+// 65,536 rows, 1,024 features by 2,048 columns from 8 bits, half precision: 307 us at the least, 344 for the median of twenty launches (895 and 798
+// TFLOP/s); the operands' way through registers (where codes become values) and the turning reads, not the products, bound it.  In floats 2,006
+// and 2,033 us, 137 and 135 of 154 TFLOP/s: there the products do.
 // The long axis is the rows: a workgroup takes BM features of dz by BN columns of a or of b and a stretch of rows, and leaves its sums in
 // 32 bits; k_lin_join adds the stretches in order.  Both operands lie with the long axis across their rows.  They are staged as
 // they lie, and the reads from LDS turn them: for 16 bits the transposing read gives lane rho of 16 lanes four rows of column rho, where

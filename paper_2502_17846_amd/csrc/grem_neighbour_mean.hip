@@ -14,7 +14,7 @@
 // the L2 too.
 // Rows of more than `segment` entries are taken apart, summed by as many waves, and joined in order: no atomics on values, the
 // same bytes on every run.
-// 1M x 128 bfloat16, 33.5M entries, 24M of them counted: 990 us; the counted rows come from beyond the L2s at 6.9 TB/s, where a kernel that does
+// 1M x 128 bfloat16, 33.5M entries, 24M of them counted: 997 us; the counted rows come from beyond the L2s at 6.9 TB/s, where a kernel that does
 // nothing but read random rows reaches 7.5.
 #include "grem_layers.hip.h"
 
