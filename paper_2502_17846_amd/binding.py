@@ -607,7 +607,7 @@ def _home(t: torch.Tensor, stream, what: str) -> int:
 
 def _at(t: torch.Tensor, here: int, what: str):
     """Returns if t is on GPU `here` and no gradient of it is lost.  (Called only where one of the two is in doubt: a call has half a dozen
-    tensors, and a look at each is 0.1 us of its 11.)"""
+    tensors; with the looks at each that is 0.4 us of its 11.)"""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
     if t.get_device() != here:

@@ -409,7 +409,7 @@ __global__ __launch_bounds__(Tile::threads) void k_lin_product(Product p, Epilog
 //
 // What bounds it is that path: 65,536 x 2,048 by 1,024 takes 208 us without the loads and 223 without the products, and took 286 with a step's
 // loads sent at once, because a wave that sends them stands until the memory pipeline has taken them all; dealt out between the
-// products 264 (1,040 TFLOP/s).  Four or five steps of 64 bytes under way are slower than two of 128 (338 and 348 us for 300).
+// products 264 to 270 (1,040 to 1,020 TFLOP/s).  Four or five steps of 64 bytes under way are slower than two of 128 (338 and 348 us for 300).
 // A workgroup takes tiles one after the other, and the next one's first steps come while one is stored.
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void mem_void;
